@@ -27,6 +27,8 @@ EXPORTS = [
     "corun_sched_enable_batched_prefill", "corun_prefill_geometry", "corun_prefill_class",
     "corun_moe_create", "corun_moe_destroy", "corun_moe_forward", "corun_moe_sync", "corun_moe_weight_bytes",
     "corun_moe_launches", "corun_mla_attend", "corun_mla_workspace_floats", "corun_mla_sync",
+    "corun_rope_create", "corun_rope_destroy", "corun_rope_apply", "corun_kv8_append", "corun_kv8_attend", "corun_kv8_attend_bytes",
+    "corun_kv8_sync", "corun_kv8_evict", "corun_kv8_evict_bytes",
 ]
 
 
@@ -56,6 +58,29 @@ class MlaLayers(C.Structure):
     """``corun_mla_layers``."""
     _fields_ = [("kv_lora_rank", C.c_int32), ("qk_nope", C.c_int32), ("qk_rope", C.c_int32), ("v_head", C.c_int32),
                 ("first_dense", C.c_int32), ("kv_norm", C.POINTER(C.c_void_p)), ("wkv_b", C.POINTER(C.c_void_p))]
+
+
+class RopeConfig(C.Structure):
+    """``corun_rope_config``."""
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32), ("original_context", C.c_int32),
+                ("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double)]
+
+
+class Heads(C.Structure):
+    """``corun_heads``."""
+    _fields_ = [("p", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Kv8CacheArgs(C.Structure):
+    """``corun_kv8_cache``."""
+    _fields_ = [("pool", C.c_void_p), ("exps", C.c_void_p), ("pages", C.c_int64), ("block", C.c_int32), ("n_kv", C.c_int32),
+                ("head_dim", C.c_int32)]
+
+
+class Kv8Rows(C.Structure):
+    """``corun_kv8_rows``."""
+    _fields_ = [("block_table", C.c_void_p), ("max_blocks", C.c_int32), ("ctx", C.c_void_p), ("cu", C.c_void_p), ("B", C.c_int32),
+                ("T", C.c_int32)]
 
 
 class CorunError(RuntimeError):
@@ -169,6 +194,19 @@ def lib():
         L.corun_moe_weight_bytes.argtypes = [vp]
         L.corun_moe_weight_bytes.restype = i64
         L.corun_moe_launches.argtypes = [vp]
+        pp = C.POINTER
+        L.corun_rope_create.argtypes = [pp(RopeConfig), pp(vp)]
+        L.corun_rope_destroy.argtypes = [vp]
+        L.corun_rope_destroy.restype = None
+        L.corun_rope_apply.argtypes = [vp, pp(Heads), pp(Heads), i32, vp, i64, i32, i32, vp]
+        L.corun_kv8_append.argtypes = [pp(Kv8CacheArgs), pp(Kv8Rows), pp(Heads), pp(Heads), i32, vp, vp, pp(Heads), pp(Heads), i32, vp, vp]
+        L.corun_kv8_attend_bytes.argtypes = [i32] * 9
+        L.corun_kv8_attend_bytes.restype = i64
+        L.corun_kv8_attend.argtypes = [pp(Kv8CacheArgs), pp(Kv8Rows), i32, pp(Heads), pp(Heads), i32, i32, C.c_float, i32, vp, vp, i64, vp]
+        L.corun_kv8_sync.argtypes = [vp, vp]
+        L.corun_kv8_evict_bytes.argtypes = [i32] * 3
+        L.corun_kv8_evict_bytes.restype = i64
+        L.corun_kv8_evict.argtypes = [pp(Kv8CacheArgs), vp, i32, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, i64, vp]
         for n in EXPORTS:
             getattr(L, n)
         _lib = L
@@ -661,6 +699,230 @@ def mla_attend(q_lat, q_rope, pool, block_table, ctx, scale: float):
     out = op.run(q_lat, q_rope, pool, block_table, ctx, scale)
     op.sync()
     return out
+
+
+ROPE_SCALINGS = ("none", "linear", "base", "parts", "bands")
+
+
+class _Device:
+    """The tensors' device as the current one while a call is made, and torch's current stream there."""
+
+    def __init__(self, t):
+        import torch
+
+        if t.device.type != "cuda":
+            raise ValueError(f"a CUDA tensor is needed, not one on {t.device}")
+        self._torch, self._index = torch, t.device.index
+        self.stream = torch.cuda.current_stream(t.device).cuda_stream
+
+    def __enter__(self):
+        self._before = self._torch.cuda.current_device()
+        if self._before != self._index:
+            self._torch.cuda.set_device(self._index)
+        return self.stream
+
+    def __exit__(self, *_):
+        if self._before != self._index:
+            self._torch.cuda.set_device(self._before)
+
+
+def _dtype_code(t, what, f32=True):
+    code = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}.get(str(t.dtype), -1)
+    if code < (0 if f32 else 1):
+        raise ValueError(f"{what}: {'float32, ' if f32 else ''}bfloat16 or float16 is needed, not {t.dtype}")
+    return code
+
+
+def _heads(t, shape, like, what):
+    """[tokens, heads, dims] with contiguous dims as a ``corun_heads``."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != like.dtype or t.device != like.device or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what}: {tuple(shape)} {like.dtype} on {like.device} with contiguous dims is needed, "
+                         f"not {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _plain(t, shape, dtype, device, what):
+    """A contiguous tensor's address."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {tuple(shape)} {dtype} on {device} is needed, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+class Rope:
+    """Rotary positions (``include/corun_rope.h``) of the first ``rot_dim`` values of every head.
+
+    ``interleaved``: pairs (2i, 2i + 1) instead of (i, i + rot_dim / 2); ``scaling``: one of ``ROPE_SCALINGS``, with
+    ``factor`` and, for "parts" and "bands", ``original_context``, ``low`` and ``high``; ``magnitude`` 0: the scaling's own."""
+
+    def __init__(self, rot_dim: int, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
+                 original_context: int = 0, low: float = 1.0, high: float = 32.0, magnitude: float = 0.0):
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling: one of {ROPE_SCALINGS} is needed, not {scaling!r}")
+        c = RopeConfig(rot_dim, int(interleaved), ROPE_SCALINGS.index(scaling), original_context, theta, factor, low, high, magnitude)
+        h = C.c_void_p()
+        self._h = None
+        _check(lib().corun_rope_create(C.byref(c), C.byref(h)), "corun_rope_create")
+        self._h, self.rot_dim = h, rot_dim
+
+    def apply(self, x, positions, out=None):
+        """x [tokens, heads, dims] (fp32, bf16 or fp16, any strides of tokens and heads), positions int32 [tokens] -> rotated
+        values in ``out`` (default: a new tensor; may be x).  Asynchronous on torch's current stream."""
+        import torch
+
+        if x.dim() != 3:
+            raise ValueError(f"x: [tokens, heads, dims] is needed, not {tuple(x.shape)}")
+        code = _dtype_code(x, "x")
+        xh = _heads(x, x.shape, x, "x")
+        y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        yh = _heads(y, x.shape, x, "out")
+        pos = _plain(positions, (x.shape[0],), torch.int32, x.device, "positions")
+        with _Device(x) as st:
+            if x.numel():
+                _check(lib().corun_rope_apply(self._h, C.byref(xh), C.byref(yh), code, pos, x.shape[0], x.shape[1], x.shape[2], st),
+                       "corun_rope_apply")
+        return y
+
+    def close(self):
+        if self._h:
+            lib().corun_rope_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Kv8Cache:
+    """One layer's keys and values in 8 bits with a power-of-two scale per page, kind and head (``include/corun_kv8.h``):
+    ``pool`` float8_e4m3fn [pages, 2, n_kv, block, head_dim] and ``exps`` int8 [pages, 2, n_kv], a value being pool * 2^exps.
+    Which pages belong to whom is the caller's to say (block tables)."""
+
+    def __init__(self, pages: int, n_kv: int, head_dim: int, block: int = 16, pool=None, exps=None, device="cuda"):
+        import torch
+
+        self._torch = torch
+        shape = (pages, 2, n_kv, block, head_dim)
+        self.pool = pool if pool is not None else torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
+        self.exps = exps if exps is not None else torch.zeros(shape[:3], dtype=torch.int8, device=self.pool.device)
+        self.pages, self.n_kv, self.head_dim, self.block = pages, n_kv, head_dim, block
+        self.device = self.pool.device
+        self._c = Kv8CacheArgs(_plain(self.pool, shape, torch.float8_e4m3fn, self.device, "pool"),
+                               _plain(self.exps, shape[:3], torch.int8, self.device, "exps"), pages, block, n_kv, head_dim)
+
+    def _rows(self, ctx, block_table, cu, T):
+        torch, dev = self._torch, self.device
+        B = ctx.shape[0]
+        if block_table.dim() != 2:
+            raise ValueError(f"block_table: [rows, blocks] is needed, not {tuple(block_table.shape)}")
+        return Kv8Rows(_plain(block_table, (B, block_table.shape[1]), torch.int32, dev, "block_table"), block_table.shape[1],
+                       _plain(ctx, (B,), torch.int32, dev, "ctx"), _plain(cu, (B + 1,), torch.int32, dev, "cu") if cu is not None else None, B, T)
+
+    def _mass(self, mass, block_table):
+        if mass is None:
+            return None
+        return _plain(mass, (block_table.shape[0], self.n_kv, block_table.shape[1] * self.block), self._torch.float32, self.device, "mass")
+
+    def append(self, k, v, ctx, block_table, cu=None, positions=None, rope: "Rope" = None, q=None, q_out=None, mass=None):
+        """Appends k, v [tokens, n_kv, head_dim]: ``ctx`` int32 [rows] counts every row's cached tokens with the new ones, ``cu``
+        int32 [rows + 1] says which tokens are whose (None: one each).  ``rope`` rotates keys and q [tokens, n_q, head_dim] at
+        ``positions`` int32 [tokens].  Returns the queries (``q_out``, or a new tensor), None without q; ``mass`` float32
+        [rows, n_kv, blocks * block]: the new tokens' accumulated weights become 0.  Asynchronous on torch's current stream."""
+        torch = self._torch
+        T = k.shape[0]
+        code = _dtype_code(k, "k")
+        if k.device != self.device:
+            raise ValueError(f"k: a tensor on {self.device} is needed, not {k.device}")
+        kh = _heads(k, (T, self.n_kv, self.head_dim), k, "k")
+        vh = _heads(v, (T, self.n_kv, self.head_dim), k, "v")
+        rows = self._rows(ctx, block_table, cu, T)
+        qh = oh = None
+        n_q = 0
+        if q is not None:
+            n_q = q.shape[1]
+            qh = _heads(q, (T, n_q, self.head_dim), k, "q")
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            oh = _heads(q_out, (T, n_q, self.head_dim), k, "q_out")
+        if rope is not None and positions is None:
+            raise ValueError("rope needs positions")
+        pos = _plain(positions, (T,), torch.int32, self.device, "positions") if positions is not None else None
+        with _Device(k) as st:
+            _check(lib().corun_kv8_append(C.byref(self._c), C.byref(rows), C.byref(kh), C.byref(vh), code, rope._h if rope is not None else None,
+                                          pos, C.byref(qh) if qh is not None else None, C.byref(oh) if oh is not None else None, n_q,
+                                          self._mass(mass, block_table), st), "corun_kv8_append")
+        return q_out if q is not None else None
+
+    def evict(self, ctx, block_table, mass, keep, max_keep: int, sinks: int = 4, recent: int = 64, new_ctx=None):
+        """Shortens every row to its first ``sinks``, its last ``recent`` and its heaviest other tokens, ``keep`` int32 [rows] (at
+        most ``max_keep``) in all, for each key head on its own.  Returns (kept int32 [rows, n_kv, max_keep]: where the tokens
+        that stayed had been, then -1; new_ctx int32 [rows]).  Asynchronous on torch's current stream."""
+        torch, dev = self._torch, self.device
+        B = ctx.shape[0]
+        rows = self._rows(ctx, block_table, None, B)
+        m = self._mass(mass, block_table)
+        if m is None:
+            raise ValueError("mass is needed")
+        kp = _plain(keep, (B,), torch.int32, dev, "keep")
+        if new_ctx is None:
+            new_ctx = torch.empty_like(ctx)
+        nc = _plain(new_ctx, (B,), torch.int32, dev, "new_ctx")
+        n_ws = int(lib().corun_kv8_evict_bytes(B, self.n_kv, max_keep))
+        kept = torch.empty((B, self.n_kv, max(max_keep, 0)), dtype=torch.int32, device=dev)
+        # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
+        ws = torch.empty(max(n_ws, 1), dtype=torch.uint8, device=dev)
+        with _Device(self.pool) as st:
+            _check(lib().corun_kv8_evict(C.byref(self._c), rows.block_table, rows.max_blocks, B, rows.ctx, nc, m, kp, max_keep, sinks, recent,
+                                         kept.data_ptr(), ws.data_ptr(), n_ws, st), "corun_kv8_evict")
+        return kept, new_ctx
+
+
+class Kv8Attention:
+    """Attention over a ``Kv8Cache`` for calls of at most ``tokens`` query tokens of ``rows`` rows, ``max_new`` a row."""
+
+    def __init__(self, rows: int, n_q: int, n_kv: int, head_dim: int, max_blocks: int, block: int = 16, tokens: int = 0, max_new: int = 1):
+        self.shape = (rows, n_q, n_kv, head_dim, max_blocks, block)
+        self.tokens, self.max_new = tokens or rows, max_new
+        self._bytes, self.ws = {}, None
+
+    def run(self, q, cache: "Kv8Cache", ctx, block_table, scale: float, cu=None, window: int = 0, mass=None, out=None):
+        """q [tokens, n_q, head_dim] (bf16 or fp16) -> out (default: a new tensor, zeros where no row writes): the rows' last cached
+        tokens' own queries, ``cu`` int32 [rows + 1] saying which are whose (None: one each).  ``window`` > 0: a query sees that
+        many tokens back, itself among them.  ``mass`` float32 [rows, n_kv, blocks * block] receives the weights.
+        Asynchronous on torch's current stream."""
+        import torch
+
+        rows, n_q, n_kv, hd, max_blocks, block = self.shape
+        T = q.shape[0]
+        code = _dtype_code(q, "q", f32=False)
+        if T > self.tokens or tuple(ctx.shape) != (rows,) or tuple(block_table.shape) != (rows, max_blocks) or q.device != cache.device or \
+                (cache.n_kv, cache.head_dim, cache.block) != (n_kv, hd, block):
+            raise ValueError(f"made for {self.tokens} tokens, {rows} rows of {max_blocks} blocks of {block} tokens, {n_kv} key heads of {hd}")
+        qh = _heads(q, (T, n_q, hd), q, "q")
+        if out is None:
+            out = torch.zeros((T, n_q, hd), dtype=q.dtype, device=q.device)
+        oh = _heads(out, (T, n_q, hd), q, "out")
+        r = cache._rows(ctx, block_table, cu, T)
+        m = cache._mass(mass, block_table)
+        L = lib()
+        key = (T, m is not None)
+        n_ws = self._bytes.get(key)
+        if n_ws is None:
+            n_ws = self._bytes[key] = int(L.corun_kv8_attend_bytes(rows, T, self.max_new, n_q, n_kv, hd, block, max_blocks, int(key[1])))
+        # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
+        ws = torch.empty(max(n_ws, 1), dtype=torch.uint8, device=q.device)
+        with _Device(q) as st:
+            _check(L.corun_kv8_attend(C.byref(cache._c), C.byref(r), self.max_new, C.byref(qh), C.byref(oh), code, n_q, float(scale), window, m,
+                                      ws.data_ptr(), n_ws, st), "corun_kv8_attend")
+        self.ws = ws
+        return out
+
+    def sync(self):
+        """Waits for the stream; raises if a bounded device-side wait of the last call expired."""
+        if self.ws is not None:
+            with _Device(self.ws) as st:
+                _check(lib().corun_kv8_sync(self.ws.data_ptr(), st), "corun_kv8_sync")
 
 
 MICROBENCH_KINDS = ("rmsnorm", "softmax", "column_sum")

@@ -1,0 +1,270 @@
+// New keys and values into the 8-bit cache (include/corun_kv8.h), with the rotation of keys and queries on the way.
+//
+// A unit is one page that a row's new tokens touch.  Its scale is set by all tokens of the page together, so one warp takes
+// a (page, key head, kind): it reads its tokens, finds the largest magnitude, settles the page's exponent, moves what the
+// page held before to it where it grew, and reads its tokens once more (from L1 by then) to store them.  The op is bound by
+// bytes (16-bit inputs in, a byte a value out, queries in and out); cos and sin, which cost some 100 instructions a pair, are
+// computed once per CTA and used for all of its heads.  Units are found from ctx and cu on the device: the launch's shape
+// depends on T and B alone, so it can be captured and replayed with other lengths.
+#include "kv8.cuh"
+
+namespace corun {
+namespace {
+
+constexpr int AP_THREADS = 256, AP_WARPS = AP_THREADS / 32;
+
+struct AppendArgs {
+  uint8_t *pool;
+  int8_t *exps;
+  long long pages;
+  int block, n_kv, n_q, B, T, max_blocks;
+  const int *block_table, *ctx, *cu, *positions;
+  const void *k, *v, *q;
+  void *q_out;
+  long long k_t, k_h, v_t, v_h, q_t, q_h, o_t, o_h;
+  float *mass;
+};
+
+// New tokens of row b and the first of them, or 0 where the row is left out.
+__device__ __forceinline__ int row_tokens(const int *ctx, const int *cu, int b, int T, long long reach, int &first, int &c) {
+  c = __ldg(ctx + b);
+  int n = 1;
+  first = b;
+  if (cu) {
+    first = __ldg(cu + b);
+    const int end = __ldg(cu + b + 1);
+    n = end - first;
+    if (first < 0 || end < first || end > T) return 0;
+  }
+  return c > 0 && n > 0 && n <= c && (long long)c <= reach ? n : 0;
+}
+
+// EPL neighbouring values of a head per lane: d0 = lane * EPL.
+template <typename T, int EPL>
+struct alignas(sizeof(T) * EPL) LanePack { T v[EPL]; };
+
+// The lane's values of one head of one token, rotated with the token's cos and sin.
+template <typename T, int HD>
+__device__ __forceinline__ void lane_values(const T *x, const float2 *cs, int rot, bool interleaved, bool packed, float (&o)[HD / 32]) {
+  constexpr int EPL = HD / 32;
+  const int d0 = (threadIdx.x & 31) * EPL;
+  if (packed) {
+    const LanePack<T, EPL> p = *reinterpret_cast<const LanePack<T, EPL> *>(x + d0);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) o[e] = to_f32(p.v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) o[e] = to_f32(x[d0 + e]);
+  }
+  if (rot == 0) return;
+  if (interleaved) {
+#pragma unroll
+    for (int e = 0; e < EPL; e += 2) {
+      if (d0 + e < rot) {
+        const float2 f = cs[(d0 + e) >> 1];
+        const float x1 = o[e], x2 = o[e + 1];
+        o[e] = x1 * f.x - x2 * f.y;
+        o[e + 1] = x2 * f.x + x1 * f.y;
+      }
+    }
+    return;
+  }
+  const int half = rot >> 1;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) {
+    const int d = d0 + e;
+    float other;
+    if (half % EPL == 0) {                        // the partner is the same value of another lane
+      const int src = (d0 < half ? d0 + half : d0 - half) / EPL;
+      other = __shfl_sync(0xffffffffu, o[e], src & 31);
+    } else {
+      other = d < rot ? to_f32(x[d < half ? d + half : d - half]) : 0.f;
+    }
+    // (with shuffles o[e] is replaced below only after every lane has read it: one e at a time, and e is its own value)
+    if (d < half) o[e] = o[e] * cs[d].x - other * cs[d].y;
+    else if (d < rot) o[e] = o[e] * cs[d - half].x + other * cs[d - half].y;
+  }
+}
+
+template <int EPL>
+__device__ __forceinline__ void store8(uint8_t *dst, const float (&x)[EPL], float f) {
+  if (EPL == 4) {
+    *reinterpret_cast<uint32_t *>(dst) = e4m3x2_of(x[0] * f, x[1] * f) | (e4m3x2_of(x[2 % EPL] * f, x[3 % EPL] * f) << 16);
+  } else {
+    *reinterpret_cast<uint16_t *>(dst) = (uint16_t)e4m3x2_of(x[0] * f, x[1] * f);
+  }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTable tab,
+                                                            int packed) {
+  constexpr int EPL = HD / 32;
+  extern __shared__ float2 cs[];                  // [tokens of the unit][rot / 2]
+  __shared__ int s_warp[AP_WARPS], s_row, s_page, s_first, s_ctx, s_n;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const long long reach = (long long)a.max_blocks * a.block;
+  if (tid == 0) s_row = -1;
+  // which row and which of its pages: units are numbered row by row
+  int before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += AP_THREADS) {
+    const int b = b0 + tid;
+    int units = 0, first = 0, c = 0, n = 0;
+    if (b < a.B) {
+      n = row_tokens(a.ctx, a.cu, b, a.T, reach, first, c);
+      if (n > 0) units = (c - 1) / a.block - (c - n) / a.block + 1;
+    }
+    int inc = units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    int ahead = before, all = 0;
+    for (int w = 0; w < AP_WARPS; ++w) { if (w < warp) ahead += s_warp[w]; all += s_warp[w]; }
+    const int lo = ahead + inc - units;
+    if ((int)blockIdx.x >= lo && (int)blockIdx.x < lo + units) {
+      s_row = b;
+      s_page = (c - n) / a.block + (int)blockIdx.x - lo;
+      s_first = first; s_ctx = c; s_n = n;
+    }
+    before += all;
+    __syncthreads();
+    if (s_row >= 0) break;
+  }
+  const int row = s_row;
+  if (row < 0) return;
+  const int jb = s_page, start = s_ctx - s_n;
+  const int z0 = max(0, start - jb * a.block), z1 = min(a.block, s_ctx - jb * a.block);   // the page's new tokens
+  const int t0 = s_first + jb * a.block + z0 - start, nt = z1 - z0;
+  const int pairs = tab.rot >> 1;
+  for (int i = tid; i < nt * pairs; i += AP_THREADS) {
+    const int t = i / pairs, p = i - t * pairs;
+    cs[i] = rope_cs(tab, p, __ldg(a.positions + t0 + t));
+  }
+  __syncthreads();
+  const long long page = __ldg(a.block_table + (long long)row * a.max_blocks + jb);
+  const bool page_ok = page >= 0 && page < a.pages;
+  const int n_task = 2 * a.n_kv + a.n_q;
+  for (int task = blockIdx.y * AP_WARPS + warp; task < n_task; task += gridDim.y * AP_WARPS) {
+    if (task < 2 * a.n_kv) {
+      const int kind = task & 1, h = task >> 1;
+      if (kind == 0 && a.mass)
+        for (int i = lane; i < nt; i += 32) a.mass[((long long)row * a.n_kv + h) * reach + (long long)jb * a.block + z0 + i] = 0.f;
+      if (!page_ok) continue;
+      const T *x = (const T *)(kind ? a.v : a.k) + (long long)t0 * (kind ? a.v_t : a.k_t) + (long long)h * (kind ? a.v_h : a.k_h);
+      const long long step = kind ? a.v_t : a.k_t;
+      const int rot = kind ? 0 : tab.rot;
+      const long long at = (page * 2 + kind) * a.n_kv + h;
+      uint8_t *dst = a.pool + at * a.block * HD + lane * EPL;
+      float mx = 0.f;
+#pragma unroll 4
+      for (int t = 0; t < nt; ++t) {
+        float o[EPL];
+        lane_values<T, HD>(x + t * step, cs + t * pairs, rot, tab.interleaved, packed, o);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) mx = fmaxf(mx, fabsf(o[e]));
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      int e_new = kv8_exp_of(mx);
+      if (z0 > 0) {
+        const int e_old = a.exps[at];
+        if (e_new > e_old) {                      // the tokens that are there already move to the larger scale
+          const float f = pow2f(max(e_old - e_new, -100));
+#pragma unroll 4
+          for (int t = 0; t < z0; ++t) {
+            if (EPL == 4) {
+              uint32_t *w = reinterpret_cast<uint32_t *>(dst + t * HD);
+              *w = e4m3x4_shift(*w, f);
+            } else {
+              uint16_t *w = reinterpret_cast<uint16_t *>(dst + t * HD);
+              const float2 v = e4m3x2_to(*w);
+              *w = (uint16_t)e4m3x2_of(v.x * f, v.y * f);
+            }
+          }
+        } else {
+          e_new = e_old;
+        }
+      }
+      __syncwarp();
+      if (lane == 0) a.exps[at] = (int8_t)e_new;
+      const float f = pow2f(-e_new);
+#pragma unroll 4
+      for (int t = 0; t < nt; ++t) {
+        float o[EPL];
+        lane_values<T, HD>(x + t * step, cs + t * pairs, rot, tab.interleaved, packed, o);
+        store8<EPL>(dst + (z0 + t) * HD, o, f);
+      }
+    } else {
+      const int h = task - 2 * a.n_kv;
+      const T *x = (const T *)a.q + (long long)t0 * a.q_t + (long long)h * a.q_h;
+      T *y = (T *)a.q_out + (long long)t0 * a.o_t + (long long)h * a.o_h;
+#pragma unroll 4
+      for (int t = 0; t < nt; ++t) {
+        float o[EPL];
+        lane_values<T, HD>(x + t * a.q_t, cs + t * pairs, tab.rot, tab.interleaved, packed, o);
+        __syncwarp();                             // (in place: every partner has been read)
+        if (packed) {
+          LanePack<T, EPL> p;
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) p.v[e] = from_f32<T>(o[e]);
+          *reinterpret_cast<LanePack<T, EPL> *>(y + t * a.o_t + lane * EPL) = p;
+        } else {
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) y[t * a.o_t + lane * EPL + e] = from_f32<T>(o[e]);
+        }
+      }
+    }
+  }
+}
+
+template <typename T>
+cudaError_t launch_append(const AppendArgs &a, const RopeTable &tab, int head_dim, bool packed, int sms, cudaStream_t st) {
+  // a row's n tokens touch at most (n - 1) / block + 2 pages, and no more than n
+  long long gx = (long long)a.T / a.block + 2ll * a.B;
+  if (gx > a.T) gx = a.T;
+  const int tasks = 2 * a.n_kv + a.n_q;
+  int gy = (int)((2ll * sms + gx - 1) / gx);
+  if (gy > (tasks + AP_WARPS - 1) / AP_WARPS) gy = (tasks + AP_WARPS - 1) / AP_WARPS;
+  const size_t smem = (size_t)a.block * (tab.rot / 2) * sizeof(float2);   // at most 32 KiB
+  const dim3 grid((unsigned)gx, (unsigned)gy);
+  if (head_dim == 128) return launch_k(append_kernel<T, 128>, grid, dim3(AP_THREADS), smem, st, false, a, tab, packed ? 1 : 0);
+  return launch_k(append_kernel<T, 64>, grid, dim3(AP_THREADS), smem, st, false, a, tab, packed ? 1 : 0);
+}
+
+}  // namespace
+}  // namespace corun
+
+using namespace corun;
+
+extern "C" int corun_kv8_append(const corun_kv8_cache *cache, const corun_kv8_rows *rows, const corun_heads *k, const corun_heads *v,
+                                int32_t dtype, const corun_rope *rope, const int32_t *positions, const corun_heads *q,
+                                const corun_heads *q_out, int32_t n_q, float *mass, void *cuda_stream) {
+  if (!kv8_cache_ok(cache) || !kv8_rows_ok(rows, cache) || !k || !v || !k->p || !v->p || dtype < CORUN_F32 || dtype > CORUN_F16) return CORUN_EINVAL;
+  const uintptr_t sz = (uintptr_t)dtype_size(dtype);
+  if (!aligned_to(k->p, sz) || !aligned_to(v->p, sz)) return CORUN_EINVAL;
+  if (q && (!q->p || !q_out || !q_out->p || n_q < 1 || n_q > 65535 || !aligned_to(q->p, sz) || !aligned_to(q_out->p, sz))) return CORUN_EINVAL;
+  if (q && q->p == q_out->p && (q->token_stride != q_out->token_stride || q->head_stride != q_out->head_stride)) return CORUN_EINVAL;
+  if (rope && (!positions || rope->t.rot > cache->head_dim)) return CORUN_EINVAL;
+  if (rows->T == 0) return CORUN_OK;
+  int dev = 0, sms = 0;
+  cudaError_t ce = cudaGetDevice(&dev);
+  if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
+  const corun_heads none{nullptr, 0, 0}, &qi = q ? *q : none, &qo = q ? *q_out : none;
+  const AppendArgs a{(uint8_t *)cache->pool, cache->exps, cache->pages, cache->block, cache->n_kv, q ? n_q : 0, rows->B, rows->T, rows->max_blocks,
+                     rows->block_table, rows->ctx, rows->cu, positions, k->p, v->p, qi.p, qo.p, k->token_stride, k->head_stride,
+                     v->token_stride, v->head_stride, qi.token_stride, qi.head_stride, qo.token_stride, qo.head_stride, mass};
+  static const RopeTable still = {};               // rot 0: nothing is rotated
+  const RopeTable &tab = rope ? rope->t : still;
+  // a lane's values (2 or 4) in one load or store where every head starts on 16 bytes
+  const bool packed = heads_on_16(*k, dtype) && heads_on_16(*v, dtype) && (!q || (heads_on_16(qi, dtype) && heads_on_16(qo, dtype)));
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (dtype == CORUN_F32) ce = launch_append<float>(a, tab, cache->head_dim, packed, sms, st);
+  else if (dtype == CORUN_BF16) ce = launch_append<__nv_bfloat16>(a, tab, cache->head_dim, packed, sms, st);
+  else ce = launch_append<__half>(a, tab, cache->head_dim, packed, sms, st);
+  if (ce != cudaSuccess) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
+  return CORUN_OK;
+}
