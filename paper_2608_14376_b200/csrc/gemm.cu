@@ -312,6 +312,21 @@ int tma_encode_2d(CUtensorMap *m, const void *base, int is_fp16, unsigned long l
   return r == CUDA_SUCCESS ? CORUN_OK : CORUN_ECUDA;
 }
 
+int tma_encode_u8_rows(CUtensorMap *m, const void *base, unsigned long long rows, int row_bytes, int box_rows) {
+  auto enc = get_encode();
+  if (!enc) { g_last_cuda_error = 99999; return CORUN_ECUDA; }
+  if (((uintptr_t)base & 15u) || (row_bytes != 64 && row_bytes != 128) || box_rows < 1 || box_rows > 256 || rows < 1) return CORUN_EINVAL;
+  cuuint64_t dims[2] = {(cuuint64_t)row_bytes, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
+  cuuint32_t box[2] = {(cuuint32_t)row_bytes, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) g_last_cuda_error = 100000 + (int)r;
+  return r == CUDA_SUCCESS ? CORUN_OK : CORUN_ECUDA;
+}
+
 int tma_encode_store_2d(CUtensorMap *m, const void *base, int is_fp32, unsigned long long rows, int cols) {
   auto enc = get_encode();
   if (!enc) { g_last_cuda_error = 99999; return CORUN_ECUDA; }

@@ -257,6 +257,8 @@ cudaError_t gemm_rows_launch(const GemmPlan &p, const CUtensorMap *tmW_override,
 // (128 bytes, 128-byte swizzle) or 16 columns (32 bytes, 32-byte swizzle).
 int tma_encode_2d(CUtensorMap *m, const void *base, int is_fp16, unsigned long long rows, int cols, int box_rows,
                   int box_cols);
+// Tensor map over rows of 64 or 128 bytes (swizzled by that width), in boxes of box_rows whole rows.
+int tma_encode_u8_rows(CUtensorMap *m, const void *base, unsigned long long rows, int row_bytes, int box_rows);
 // Tensor map over fp16 data seen as a 4-dimensional array: dims[0] elements are contiguous, strides[i] is the byte
 // distance between consecutive indices of dimension i + 1 (a multiple of 16; they need not ascend); the box's
 // innermost extent is 64 elements (128 bytes, 128-byte swizzle).  The box lands in shared memory densely,

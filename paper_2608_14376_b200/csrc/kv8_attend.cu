@@ -1,7 +1,33 @@
-// Attention over the 8-bit cache (include/corun_kv8.h): out = softmax(scale q K^T) V, and the weights that the cached tokens received.
+// Attention over the 8-bit cache (include/corun_kv8.h): out = softmax(scale q K^T) V, and the weights that the cached tokens
+// received, on tcgen05 / TMEM / TMA (sm_100a) straight from the 8-bit pages.
 //
-// One warp per (token, query head): a lane holds head_dim / 32 dims, the cached tokens are taken one after the other with a
-// running maximum and sum.  A second kernel, one thread per cached token, forms the scores again and adds up the weights.
+// The cached tokens are the M side of both products and the query columns (query tokens x query heads of a key head, at most
+// 32 a tile) the N side, so that the cache's bytes are MMA operands as they lie in memory: no value of K or V passes
+// through a register.
+//   scores   S^T [128 tokens x 3 C] = K [128 x hd] * Q^T        K K-major, 32 values of a row per MMA
+//   output   O^T [hd x 3 C]         = V^T [hd x 128] * P^T      V read as the MN-major A operand
+// kind::f8f6f4 wants 8-bit operands on both sides.  A query (16 bits) or a weight (11 bits, fp16) is the sum of three e4m3
+// values, x = h0 + h1 / 16 + h2 / 256, each the rounding of what the ones before left (4 bits each: exact for 11 bits and
+// for bf16), and takes three columns; with few columns an MMA costs the same whatever N is, so the three are free.  Queries are
+// brought to [128, 256) by a power of two per column, weights to at most 256.
+// The scales 2^e of a token's keys multiply its scores.  Those of its values go into its weight: the product takes
+// w = 2^(s + e_v - M), M the largest s + e_v of the column in the tile, so that what is rounded is rounded relative to its
+// share in the result; the sum of weights takes w 2^-e_v back.
+// A tile's output stays in its own frame M; it is added to the running output, held in registers, in 32 bits.
+//
+// An item is (row, tile of query columns, key head, split).  Rows with one new token, or few (n G <= 16), are split into
+// at most AT_SPLITS parts of at least two tiles; rows with more are not.  The split depends on the row's own ctx, n and window alone, sums
+// have one fixed order, and which CTA computes an item has no influence on any value: a row's result does not depend on
+// the other rows.  Every CTA (one per SM) takes a stretch of the item list, cut by cost.
+//   warp 0        producer: block-table lookups, TMA loads, exponents
+//   warp 1        issues the MMAs: the scores of tile n + 1 before the output product of tile n
+//   warps 2, 3    query tile of the next item
+//   warps 4-7, 8-11   softmax of even / odd tiles, a thread per cached token
+//   warps 12-15   output: a thread per value dim
+// A second kernel combines a row's splits in ascending order, a third one adds up the weights from the scores that the
+// first wrote (4 bytes per token and column, where mass is wanted).  Every wait is bounded.
+#include <atomic>
+
 #include <math_constants.h>
 
 #include "kv8.cuh"
@@ -9,122 +35,770 @@
 namespace corun {
 namespace {
 
-constexpr int AT_MAXB = 1024;
+constexpr int AT_MAXB = 1024;       // rows per call
+constexpr int AT_T = 128;           // tokens per tile
+constexpr int AT_SPLITS = 64;       // splits of a row at most
+constexpr int AT_MIN_TILES = 2;     // tiles of a split at least
+constexpr int AT_FEW = 16;          // columns up to which a row with several new tokens is split
+constexpr int AT_MAXC = 32;         // columns of a tile at most
+constexpr int AT_RING = 4;          // K tiles, and as many V tiles, in flight
+constexpr int AT_THREADS = 512;
+constexpr int AT_STATUS = 256;      // status words at the start of the workspace
+constexpr float AT_LOW = -1e30f;    // a maximum over nothing
 
 struct AttendArgs {
-  const uint8_t *pool;
   const int8_t *exps;
   long long pages;
-  int block, n_kv, n_q, B, T, max_blocks, max_new, window;
+  int block, n_kv, n_q, B, T, max_blocks, max_new, window, cols, max_splits;   // cols: columns per (row, key head) in the workspace
   const int *block_table, *ctx, *cu;
   const void *q;
   void *out;
   long long q_t, q_h, o_t, o_h;
-  float scale;
+  float scale_log2e;
   float *mass;
-  float2 *ml;   // [T][n_q]
+  int *status;
+  float2 *part_ml;    // [B][n_kv][max_splits][cols]: frame, sum
+  float *part_o;      // [B][n_kv][max_splits][cols][hd]
+  float2 *ml;         // [B][n_kv][cols]: frame, 1 / sum (with mass)
+  float *scores;      // [B][n_kv][tokens padded to tiles][cols] (with mass)
+  long long score_tokens;
 };
 
-__device__ __forceinline__ int row_of(const AttendArgs &a, int t, int &first, int &n) {
-  if (!a.cu) { first = t; n = 1; return t < a.B ? t : -1; }
-  for (int b = 0; b < a.B; ++b) {
-    first = a.cu[b];
-    n = a.cu[b + 1] - first;
-    if (first >= 0 && t >= first && t < first + n && first + n <= a.T) return b;
+// What a row asks for: its new tokens (0 = left out), the tiles it reads, its splits.
+struct RowPlan {
+  int c, n, first, t_lo, t_hi, ns, tps, qt;   // ns splits of tps tiles; qt query tiles
+};
+__host__ __device__ inline int at_ceil(int a, int b) { return (a + b - 1) / b; }
+__device__ __forceinline__ RowPlan row_plan(int c, int first, int end, const AttendArgs &a, int G, int TQ) {
+  RowPlan r;
+  r.c = c;
+  r.first = first;
+  r.n = end - first;
+  const bool ok = c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && r.n > 0 && r.n <= a.max_new && end <= a.T;
+  if (!ok) { r.n = 0; r.ns = 0; r.qt = 0; r.t_lo = r.t_hi = 0; r.tps = 1; return r; }
+  r.t_lo = a.window ? max(0, c - r.n - a.window + 1) / AT_T : 0;
+  r.t_hi = at_ceil(c, AT_T);
+  const int nt = r.t_hi - r.t_lo;
+  if (r.n == 1 || r.n * G <= AT_FEW) {
+    r.qt = 1;
+    r.tps = max(AT_MIN_TILES, at_ceil(nt, AT_SPLITS));
+    r.ns = at_ceil(nt, r.tps);
+  } else {
+    r.qt = at_ceil(r.n, TQ);
+    r.tps = nt;
+    r.ns = 1;
   }
-  return -1;
+  return r;
 }
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(128) attend_simple_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int EPL = HD / 32;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int t = blockIdx.x, hq = blockIdx.y * 4 + warp;
-  if (hq >= a.n_q) return;
-  int first, n;
-  const int b = row_of(a, t, first, n);
-  if (b < 0) return;
-  const long long reach = (long long)a.max_blocks * a.block;
-  const int c = a.ctx[b];
-  if (c <= 0 || c > reach || n > a.max_new) return;
-  const int g = hq / (a.n_q / a.n_kv), self = c - n + (t - first);
-  float q[EPL], o[EPL];
-#pragma unroll
-  for (int e = 0; e < EPL; ++e) { q[e] = to_f32(((const T *)a.q)[t * a.q_t + hq * a.q_h + lane * EPL + e]) * a.scale; o[e] = 0.f; }
-  float m = -CUDART_INF_F, l = 0.f;
-  for (int j = a.window ? max(0, self - a.window + 1) : 0; j <= self; ++j) {
-    const long long page = a.block_table[(long long)b * a.max_blocks + j / a.block];
-    float k[EPL], v[EPL];
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) k[e] = v[e] = 0.f;
-    if (page >= 0 && page < a.pages) {
-      const long long ak = (page * 2) * a.n_kv + g, av = ak + a.n_kv;
-      const uint8_t *pk = a.pool + (ak * a.block + j % a.block) * HD + lane * EPL, *pv = a.pool + (av * a.block + j % a.block) * HD + lane * EPL;
-      const float fk = pow2f(a.exps[ak]), fv = pow2f(a.exps[av]);
-#pragma unroll
-      for (int e = 0; e < EPL; e += 2) {
-        const float2 x = e4m3x2_to(*(const uint16_t *)(pk + e)), y = e4m3x2_to(*(const uint16_t *)(pv + e));
-        k[e] = x.x * fk; k[e + 1] = x.y * fk; v[e] = y.x * fv; v[e + 1] = y.y * fv;
-      }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Rows of 64 bytes with the 64-byte swizzle: groups of eight rows are 512 bytes; layout type 4.  K-major and, with one
+// block of 64 M elements, MN-major tiles alike (the stride byte offset is the distance of groups of eight rows in both).
+__device__ __forceinline__ uint64_t desc_sw64(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr >> 4) & 0x3FFFu);
+  d |= (uint64_t)1u << 16;
+  d |= (uint64_t)(512u >> 4) << 32;
+  d |= (uint64_t)1u << 46;
+  d |= (uint64_t)4u << 61;
+  return d;
+}
+template <int HD>
+__device__ __forceinline__ uint64_t desc_hd(uint32_t smem_addr) { return HD == 128 ? umma_desc_sw128(smem_addr) : desc_sw64(smem_addr); }
+// Byte b of row r of a swizzled tile with rows of W bytes (128: chunk ^ row mod 8, 64: chunk ^ row / 2 mod 4).
+template <int W>
+__device__ __forceinline__ uint32_t swz(int r, int b) {
+  return W == 128 ? (uint32_t)(r * 128 + ((((b >> 4) ^ (r & 7)) << 4) | (b & 15))) : (uint32_t)(r * 64 + ((((b >> 4) ^ ((r >> 1) & 3)) << 4) | (b & 15)));
+}
+
+// An item of the list.
+struct Item {
+  int b, g, split, i0, ni, t0, t1;   // row, key head, split, first query token of the tile, their number, tiles [t0, t1)
+};
+
+template <int C>
+struct Smem {
+  uint64_t k_full[AT_RING], k_empty[AT_RING], v_full[AT_RING], v_empty[AT_RING];
+  uint64_t q_ready, q_free, s_full[2], s_free[2], p_ready[2], p_free[2], o_full[2], o_free[2], e_full[2], e_free[2], x_bar[2], l_ready[2], l_free[2];
+  uint32_t tmem;
+  int abort_flag;
+  int my_items[2];
+  float q_mul[4][C];                 // 2^e of a query column times scale log2(e), by query tile
+  float x_max[2][2][C][4];           // [group][use parity][column][warp]: maxima of 32 tokens
+  float frame[2][C];                 // [tile parity]: the tile's frames
+  float2 ab[12][C];                  // [warp - 4]: factors of old and new of every column
+  float lpart[2][8][C];              // [item parity][group * 4 + warp]: sums of weights
+  float lframe[2][2][C];             // [item parity][group]: their frames
+  int8_t exps[2][2][8];              // [tile parity][kind][page of the tile]
+  int row_item[AT_MAXB + 1];         // first item of every row
+  int row_ic[AT_MAXB + 1];           // cost of one of its items
+  long long row_cost[AT_MAXB + 1];   // cost of the items before the row
+};
+
+template <int HD, int C>
+constexpr int smem_bytes() { return 2 * AT_RING * AT_T * HD + (C == 4 ? 16 : C == 8 ? 32 : 3 * C) * (HD + 2 * AT_T) + (int)sizeof(Smem<C>) + 2048; }
+
+template <typename T, int HD, int C>
+__global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ AttendArgs a) {
+  constexpr int N = C == 4 ? 16 : C == 8 ? 32 : 3 * C;          // an M = 128 MMA takes N in steps of 16
+  constexpr int TILE = AT_T * HD;
+  constexpr uint32_t TMEM_COLS = 4 * N <= 64 ? 64 : 4 * N <= 128 ? 128 : 4 * N <= 256 ? 256 : 512;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t *base_ptr = smem_raw + (base - smem_u32(smem_raw));
+  // [K ring][V ring][query tile][two weight tiles][the rest]: tiles start on 1 KiB (the query tile's size is a multiple of it)
+  const uint32_t k_ring = base, v_ring = base + AT_RING * TILE, q_tile = base + 2 * AT_RING * TILE, p_tile = q_tile + (uint32_t)((N * HD + 1023) & ~1023);
+  uint8_t *q_ptr = base_ptr + (q_tile - base), *p_ptr = base_ptr + (p_tile - base);
+  Smem<C> &sm = *reinterpret_cast<Smem<C> *>(p_ptr + 2 * N * AT_T);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.n_q / a.n_kv, TQ = C / G;
+
+  if (tid == 0) {
+    sm.abort_flag = 0;
+    for (int s = 0; s < AT_RING; ++s) {
+      mbar_init(smem_u32(&sm.k_full[s]), 1); mbar_init(smem_u32(&sm.k_empty[s]), 1);
+      mbar_init(smem_u32(&sm.v_full[s]), 1); mbar_init(smem_u32(&sm.v_empty[s]), 1);
     }
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) s = fmaf(q[e], k[e], s);
-#pragma unroll
-    for (int i = 16; i > 0; i >>= 1) s += __shfl_xor_sync(0xffffffffu, s, i);
-    const float m2 = fmaxf(m, s), f = expf(m - m2), p = expf(s - m2);
-    l = l * f + p;
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) o[e] = o[e] * f + p * v[e];
-    m = m2;
+    mbar_init(smem_u32(&sm.q_ready), 2);
+    mbar_init(smem_u32(&sm.q_free), 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&sm.s_full[s]), 1); mbar_init(smem_u32(&sm.s_free[s]), 4);
+      mbar_init(smem_u32(&sm.p_ready[s]), 4); mbar_init(smem_u32(&sm.p_free[s]), 1);
+      mbar_init(smem_u32(&sm.o_full[s]), 1); mbar_init(smem_u32(&sm.o_free[s]), 4);
+      mbar_init(smem_u32(&sm.e_full[s]), 1); mbar_init(smem_u32(&sm.e_free[s]), 4);
+      mbar_init(smem_u32(&sm.x_bar[s]), 4);
+      mbar_init(smem_u32(&sm.l_ready[s]), 8); mbar_init(smem_u32(&sm.l_free[s]), 4);
+    }
+    fence_mbar_init();
+    fence_proxy_async();
+    prefetch_tensormap(&tm);
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  if (warp == 0) {
+    tmem_alloc(smem_u32(&sm.tmem), TMEM_COLS);
+    tmem_relinquish();
+  } else if (warp >= 4) {
+    // operand rows that no column writes stay zero
+    uint4 *z = reinterpret_cast<uint4 *>(q_ptr);
+    for (int i = tid - 128; i < (int)(p_tile - q_tile + 2 * N * AT_T) / 16; i += AT_THREADS - 128) z[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async();
+  } else if (warp == 2) {
+    // the item list: how many items, and what they cost, before every row
+    int run = 0;
+    long long crun = 0;
+    for (int r0 = 0; r0 < a.B; r0 += 32) {
+      const int r = r0 + lane;
+      int n = 0;
+      long long cst = 0;
+      if (r < a.B) {
+        const int first = a.cu ? __ldg(a.cu + r) : r, end = a.cu ? __ldg(a.cu + r + 1) : r + 1;
+        const RowPlan p = row_plan(__ldg(a.ctx + r), first, end, a, G, TQ);
+        n = p.qt * p.ns * a.n_kv;                     // 0 for a row that is left out
+        // a tile's cost is 2, an item's beyond its tiles 1; with several query tiles the first see fewer tokens
+        const int ic = 1 + 2 * (p.qt > 1 ? max(1, (p.c - p.n / 2) / AT_T + 1 - p.t_lo) : p.tps);
+        sm.row_ic[r] = ic;
+        cst = (long long)n * ic;
+      }
+      int inc = n;
+      long long cinc = cst;
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) ((T *)a.out)[t * a.o_t + hq * a.o_h + lane * EPL + e] = from_f32<T>(o[e] * inv);
-  if (lane == 0 && a.ml) a.ml[(long long)t * a.n_q + hq] = make_float2(m, inv);
-}
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, o);
+        const long long cv = __shfl_up_sync(0xffffffffu, cinc, o);
+        if (lane >= o) { inc += v; cinc += cv; }
+      }
+      if (r < a.B) { sm.row_item[r] = run + inc - n; sm.row_cost[r] = crun + cinc - cst; }
+      run += __shfl_sync(0xffffffffu, inc, 31);
+      crun += __shfl_sync(0xffffffffu, cinc, 31);
+    }
+    __syncwarp();
+    if (lane == 0) {
+      sm.row_item[a.B] = run;
+      sm.row_cost[a.B] = crun;
+      auto bound = [&](int k) {                       // an item goes to the CTA in whose share of the cost it starts
+        if (k >= (int)gridDim.x) return run;
+        const long long t = (crun * k + gridDim.x - 1) / gridDim.x;
+        int lo = 0, hi = a.B;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (sm.row_cost[mid] <= t) lo = mid; else hi = mid;
+        }
+        const long long i = (t - sm.row_cost[lo] + sm.row_ic[lo] - 1) / sm.row_ic[lo];
+        return (int)min((long long)sm.row_item[lo] + i, (long long)sm.row_item[lo + 1]);
+      };
+      sm.my_items[0] = bound((int)blockIdx.x);
+      sm.my_items[1] = bound((int)blockIdx.x + 1);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t s_tmem = sm.tmem, o_tmem = s_tmem + 2 * N;
+  const int item_lo = sm.my_items[0], item_hi = sm.my_items[1];
+  bool failed = false;
+  int cur = -1;
+  RowPlan rp = {};
+  auto locate = [&](int it) {                         // items ascend: the row pointer only moves forward
+    bool moved = cur < 0;
+    if (moved) cur = 0;
+    while (it >= sm.row_item[cur + 1]) { ++cur; moved = true; }
+    if (moved) rp = row_plan(__ldg(a.ctx + cur), a.cu ? __ldg(a.cu + cur) : cur, a.cu ? __ldg(a.cu + cur + 1) : cur + 1, a, G, TQ);
+    Item x;
+    const int i = it - sm.row_item[cur], unit = i / rp.ns, qt = unit % rp.qt;
+    x.b = cur;
+    x.split = i - unit * rp.ns;
+    x.g = unit / rp.qt;
+    x.i0 = qt * TQ;
+    x.ni = min(TQ, rp.n - x.i0);
+    if (rp.qt > 1 || rp.ns == 1) {                    // whole range of the tile's own queries
+      const int lim0 = rp.c - rp.n + x.i0, lim1 = lim0 + x.ni - 1;
+      x.t0 = a.window ? max(0, lim0 - a.window + 1) / AT_T : 0;
+      x.t1 = max(x.t0 + 1, lim1 < 0 ? 0 : lim1 / AT_T + 1);
+    } else {
+      x.t0 = rp.t_lo + x.split * rp.tps;
+      x.t1 = min(rp.t_hi, x.t0 + rp.tps);
+    }
+    return x;
+  };
+  auto same_query = [](const Item &x, const Item &y) { return x.b == y.b && x.g == y.g && x.i0 == y.i0; };
+  auto wait_all = [&](uint64_t &bar, uint32_t parity) {   // by a whole warp
+    const bool ok = mbar_wait(smem_u32(&bar), parity & 1u, &sm.abort_flag);
+    if (!__all_sync(0xffffffffu, ok)) failed = true;
+    return !failed;
+  };
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(128) attend_mass_simple_kernel(const __grid_constant__ AttendArgs a) {
-  const int b = blockIdx.x / a.n_kv, g = blockIdx.x - b * a.n_kv, G = a.n_q / a.n_kv;
-  const long long reach = (long long)a.max_blocks * a.block;
-  const int c = a.ctx[b];
-  if (c > reach) return;
-  const int first = a.cu ? a.cu[b] : b, n = a.cu ? a.cu[b + 1] - first : 1;
-  if (n > a.max_new || first < 0 || first + n > a.T) return;
-  for (int j = blockIdx.y * 128 + threadIdx.x; j < c; j += gridDim.y * 128) {
-    const long long page = a.block_table[(long long)b * a.max_blocks + j / a.block];
-    float sum = 0.f;
-    for (int i = 0; i < n; ++i) {
-      const int self = c - n + i;
-      if (j > self || (a.window && j <= self - a.window)) continue;
-      for (int h = 0; h < G; ++h) {
-        const int hq = g * G + h;
-        float s = 0.f;
-        if (page >= 0 && page < a.pages) {
-          const long long ak = (page * 2) * a.n_kv + g;
-          const uint8_t *pk = a.pool + (ak * a.block + j % a.block) * HD;
-          const float fk = pow2f(a.exps[ak]);
-          const T *q = (const T *)a.q + (first + i) * a.q_t + hq * a.q_h;
-          for (int d = 0; d < HD; d += 2) {
-            const float2 x = e4m3x2_to(*(const uint16_t *)(pk + d));
-            s = fmaf(to_f32(q[d]) * a.scale, x.x * fk, s);
-            s = fmaf(to_f32(q[d + 1]) * a.scale, x.y * fk, s);
+  if (warp == 0) {
+    // ---------------- producer ----------------
+    const uint64_t pol = l2_policy_evict_normal();
+    const int per = AT_T / a.block;                   // pages of a tile: lane l looks after page l
+    int n = 0;
+    int it = item_lo, t = 0;
+    Item x = {};
+    // a cursor one tile ahead: its pages are looked up while the tile before is loaded
+    auto page_of = [&](const Item &y, int tile) {
+      const int j = tile * per + lane;
+      return lane < per && j * a.block < rp.c ? __ldg(a.block_table + (size_t)y.b * a.max_blocks + j) : -1;
+    };
+    int page = -1;
+    if (it < item_hi) { x = locate(it); t = x.t0; page = page_of(x, t); }
+    while (it < item_hi && !failed) {
+      // this tile
+      const int c = rp.c, g = x.g;
+      const int np = min(per, at_ceil(c - t * AT_T, a.block));
+      const bool page_ok = page >= 0 && (long long)page < a.pages;
+      const long long at = ((long long)page * 2) * a.n_kv + g;
+      int ek = 0, ev = 0;
+      if (lane < np && page_ok) { ek = __ldg(a.exps + at); ev = __ldg(a.exps + at + a.n_kv); }
+      const int y_none = (int)(a.pages * 2 * a.n_kv * a.block);       // behind the pool: a page outside of it reads as zeros
+      const int yk = page_ok ? (int)(at * a.block) : y_none, yv = page_ok ? (int)((at + a.n_kv) * a.block) : y_none;
+      // the next tile's pages
+      if (++t >= x.t1) {
+        if (++it < item_hi) { x = locate(it); t = x.t0; }
+      }
+      page = it < item_hi ? page_of(x, t) : -1;
+      const int s = n % AT_RING;
+      const uint32_t bytes = (uint32_t)(np * a.block * HD);
+      if (n >= AT_RING && !wait_all(sm.k_empty[s], (uint32_t)(n / AT_RING - 1))) break;
+      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.k_full[s]), bytes);
+      __syncwarp();
+      if (lane < np) tma_load_2d(k_ring + (uint32_t)(s * TILE + lane * a.block * HD), &tm, 0, yk, smem_u32(&sm.k_full[s]), pol);
+      if (n >= AT_RING && !wait_all(sm.v_empty[s], (uint32_t)(n / AT_RING - 1))) break;
+      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.v_full[s]), bytes);
+      __syncwarp();
+      if (lane < np) tma_load_2d(v_ring + (uint32_t)(s * TILE + lane * a.block * HD), &tm, 0, yv, smem_u32(&sm.v_full[s]), pol);
+      if (n >= 2 && !wait_all(sm.e_free[n & 1], (uint32_t)(n / 2 - 1))) break;
+      if (lane < 8) { sm.exps[n & 1][0][lane] = (int8_t)ek; sm.exps[n & 1][1][lane] = (int8_t)ev; }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.e_full[n & 1]));
+      ++n;
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer ----------------
+    if (elect_one()) {
+      // D fp32, A and B e4m3 (format 0); scores: M = 128; output: M = hd, A MN-major
+      const uint32_t idesc_s = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(AT_T >> 4) << 24);
+      const uint32_t idesc_o = (1u << 4) | (1u << 15) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(HD >> 4) << 24);
+      auto wait = [&](uint64_t &bar, uint32_t parity) {
+        if (!mbar_wait(smem_u32(&bar), parity & 1u, &sm.abort_flag)) failed = true;
+        return !failed;
+      };
+      auto output = [&](int n) {                      // the product of tile n's weights and values
+        const int s = n % AT_RING, h = n & 1;
+        if (!wait(sm.p_ready[h], (uint32_t)(n / 2)) || !wait(sm.v_full[s], (uint32_t)(n / AT_RING))) return;
+        if (n >= 2 && !wait(sm.o_free[h], (uint32_t)(n / 2 - 1))) return;
+        tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < AT_T / 32; ++k) {
+          const uint64_t da = (HD == 128 ? umma_desc_sw128_mn(v_ring + (uint32_t)(s * TILE), 1024u, 1024u) : desc_sw64(v_ring + (uint32_t)(s * TILE))) +
+                              (uint64_t)(k * 32 * HD / 16);
+          const uint64_t db = umma_desc_sw128(p_tile + (uint32_t)(h * N * AT_T)) + (uint64_t)(k * 2);
+          umma_f8(o_tmem + (uint32_t)(h * N), da, db, idesc_o, k > 0 ? 1u : 0u);
+        }
+        umma_commit(smem_u32(&sm.v_empty[s]));
+        umma_commit(smem_u32(&sm.p_free[h]));
+        umma_commit(smem_u32(&sm.o_full[h]));
+      };
+      int n = 0, n_q = 0;
+      Item x = {}, last = {};
+      for (int it = item_lo; it < item_hi && !failed; ++it) {
+        x = locate(it);
+        if (it == item_lo || !same_query(x, last)) {
+          if (it > item_lo) umma_commit(smem_u32(&sm.q_free));        // every score product of the tile before has been issued
+          if (!wait(sm.q_ready, (uint32_t)n_q)) break;
+          ++n_q;
+        }
+        last = x;
+        for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
+          const int s = n % AT_RING, h = n & 1;
+          if (!wait(sm.k_full[s], (uint32_t)(n / AT_RING))) break;
+          if (n >= 2 && !wait(sm.s_free[h], (uint32_t)(n / 2 - 1))) break;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < HD / 32; ++k)
+            umma_f8(s_tmem + (uint32_t)(h * N), desc_hd<HD>(k_ring + (uint32_t)(s * TILE)) + (uint64_t)(k * 2), desc_hd<HD>(q_tile) + (uint64_t)(k * 2),
+                    idesc_s, k > 0 ? 1u : 0u);
+          umma_commit(smem_u32(&sm.k_empty[s]));
+          umma_commit(smem_u32(&sm.s_full[h]));
+          if (n > 0) output(n - 1);
+        }
+      }
+      if (n > 0 && !failed) output(n - 1);
+    }
+  } else if (warp < 4) {
+    // ---------------- query tile ----------------
+    // row piece * C + column, hd bytes, swizzled as the keys are; a warp per column, hd / 32 values a lane
+    constexpr int EPL = HD / 32;
+    int n_q = 0;
+    Item x = {}, last = {};
+    for (int it = item_lo; it < item_hi && !failed; ++it) {
+      x = locate(it);
+      if (it > item_lo && same_query(x, last)) continue;
+      last = x;
+      if (n_q > 0 && !wait_all(sm.q_free, (uint32_t)(n_q - 1))) break;
+      const int cols = x.ni * G;
+      for (int c = warp - 2; c < cols; c += 2) {
+        const T *src = (const T *)a.q + (long long)(rp.first + x.i0 + c / G) * a.q_t + (long long)(x.g * G + c % G) * a.q_h + lane * EPL;
+        float v[EPL];
+        if (EPL == 4) {
+          const uint2 u = __ldg(reinterpret_cast<const uint2 *>(src));
+          const T *e = reinterpret_cast<const T *>(&u);
+#pragma unroll
+          for (int i = 0; i < EPL; ++i) v[i] = to_f32(e[i]);
+        } else {
+          const uint32_t u = __ldg(reinterpret_cast<const uint32_t *>(src));
+          const T *e = reinterpret_cast<const T *>(&u);
+#pragma unroll
+          for (int i = 0; i < EPL; ++i) v[i] = to_f32(e[i]);
+        }
+        float mx = 0.f;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+          if (!(fabsf(v[i]) <= 3.4e38f)) v[i] = CUDART_NAN_F;        // an infinite query makes its scores NaN
+          mx = fmaxf(mx, fabsf(v[i]));
+        }
+        mx = warp_max(mx);
+        // to [128, 256): e from the exponent bits (a subnormal maximum counts as 2^-126)
+        const int e = max((__float_as_int(mx) >> 23) - 127, -110) - 7;
+        const float down = pow2f(-e > 126 ? 126 : -e);
+        uint32_t w[3] = {0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < EPL; i += 2) {
+          float r0 = v[i] * down, r1 = v[i + 1] * down;
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+            const uint32_t h = e4m3x2_of(r0, r1);
+            const float2 f = e4m3x2_to(h);
+            r0 = (r0 - f.x) * 16.f;
+            r1 = (r1 - f.y) * 16.f;
+            w[p] |= h << (8 * i);
           }
         }
-        const float2 ml = a.ml[(long long)(first + i) * a.n_q + hq];
-        sum += expf(s - ml.x) * ml.y;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          uint8_t *dst = q_ptr + swz<HD>(p * C + c, lane * EPL);
+          if (EPL == 4) *reinterpret_cast<uint32_t *>(dst) = w[p]; else *reinterpret_cast<uint16_t *>(dst) = (uint16_t)w[p];
+        }
+        if (lane == 0) sm.q_mul[n_q & 3][c] = (mx > 0.f ? pow2f(e) : 1.f) * a.scale_log2e;
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.q_ready));
+      ++n_q;
+    }
+  } else if (warp < 12) {
+    // ---------------- softmax: group 0 takes the even tiles, group 1 the odd ones ----------------
+    const int grp = warp >= 8 ? 1 : 0, wq = warp & 3, tok = wq * 32 + lane;
+    const uint32_t s_lane = s_tmem + ((uint32_t)(32 * wq) << 16) + (uint32_t)(grp * N);
+    float2 *ab = sm.ab[warp - 4];
+    float l[C];
+    float m_run = AT_LOW;                             // lane c: the running frame of column c
+    int n = 0, n_q = -1, k = 0;                       // k: tiles this group has done
+    Item x = {}, last = {};
+    for (int it = item_lo; it < item_hi && !failed; ++it) {
+      x = locate(it);
+      if (it == item_lo || !same_query(x, last)) ++n_q;
+      last = x;
+      const int cols = x.ni * G;
+#pragma unroll
+      for (int c = 0; c < C; ++c) l[c] = 0.f;
+      m_run = AT_LOW;
+      const int lim0 = rp.c - rp.n + x.i0, lim1 = lim0 + x.ni - 1;
+      for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
+        if ((n & 1) != grp) continue;
+        const int j = t * AT_T + tok;
+        if (!wait_all(sm.e_full[grp], (uint32_t)k)) break;
+        const int pg = tok / a.block;
+        const float ek = pow2f(sm.exps[grp][0][pg]);
+        const int ev_i = sm.exps[grp][1][pg];
+        const float ev = (float)ev_i;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.e_free[grp]));
+        if (!wait_all(sm.s_full[grp], (uint32_t)k)) break;
+        tc_fence_after();
+        const bool masked = (t + 1) * AT_T > lim0 + 1 || (a.window && t * AT_T <= lim1 - a.window);
+        const float *qm = sm.q_mul[n_q & 3];
+        float y[C];
+        float *sc = a.mass ? a.scores + (((long long)x.b * a.n_kv + x.g) * a.score_tokens + j) * a.cols : nullptr;
+        bool unseen = true;                           // no column sees the token
+#pragma unroll
+        for (int c0 = 0; c0 < C; c0 += 16) {
+          uint32_t v[3 * (C < 16 ? C : 16)];
+          constexpr int W = C < 16 ? C : 16;
+          if (C == 4) {
+            tmem_ld8(s_lane, *reinterpret_cast<uint32_t(*)[8]>(&v[0]));
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]) : "r"(s_lane + 8) : "memory");
+          } else if (C == 8) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) tmem_ld8(s_lane + (uint32_t)(p * C), *reinterpret_cast<uint32_t(*)[8]>(&v[p * W]));
+          } else {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) tmem_ld16(s_lane + (uint32_t)(p * C + c0), *reinterpret_cast<uint32_t(*)[16]>(&v[(p * W) % (3 * W)]));
+          }
+          tmem_ld_wait();
+#pragma unroll
+          for (int c = 0; c < W; ++c) {
+            const float s = fmaf(__uint_as_float(v[2 * W + c]), 1.f / 256.f, fmaf(__uint_as_float(v[W + c]), 1.f / 16.f, __uint_as_float(v[c])));
+            y[c0 + c] = s * (ek * qm[c0 + c]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.s_free[grp]));
+        if (masked) {
+          int h = 0, lim = lim0;
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const bool see = j <= lim && !(a.window && j <= lim - a.window);
+            if (c < cols && see) unseen = false;
+            if (!see) y[c] = -CUDART_INF_F;
+            if (++h == G) { h = 0; ++lim; }
+          }
+        } else {
+          unseen = false;
+        }
+        if (sc) {
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (c < cols) sc[c] = y[c];
+        }
+        // the tile's frame: the largest s + e_v of every column
+        float (*xm)[4] = sm.x_max[grp][k & 1];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          y[c] += ev;
+          const float mx = warp_max(y[c]);
+          if (lane == 0) xm[c][wq] = mx;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.x_bar[grp]));
+        if (!wait_all(sm.x_bar[grp], (uint32_t)k)) break;
+        // lane c: the column's frame and what the running sum and this tile's are multiplied by
+        float m_tile = AT_LOW;
+        if (lane < C) {
+          const float4 f = *reinterpret_cast<const float4 *>(xm[lane]);
+          m_tile = fmaxf(fmaxf(fmaxf(f.x, f.y), fmaxf(f.z, f.w)), AT_LOW);
+          const float m_new = fmaxf(m_run, m_tile);
+          ab[lane] = make_float2(ex2(m_run - m_new), ex2(m_tile - m_new));
+          m_run = m_new;
+        }
+        // P of the tile before the last must have been read, and its frames
+        if (k > 0 && !wait_all(sm.p_free[grp], (uint32_t)(k - 1))) break;
+        if (k > 0 && !wait_all(sm.o_free[grp], (uint32_t)(k - 1))) break;
+        if (wq == 0 && lane < C) sm.frame[grp][lane] = m_tile;
+        __syncwarp();
+        uint8_t *p_row = p_ptr + grp * N * AT_T;
+        const float back = pow2f(-ev_i);
+        float m_all = m_tile;
+#pragma unroll
+        for (int c = 0; c < C; c += 2) {
+          const float m0 = __shfl_sync(0xffffffffu, m_all, c), m1 = __shfl_sync(0xffffffffu, m_all, c + 1);
+          const float w0 = ex2(y[c] - m0 + 8.f), w1 = ex2(y[c + 1] - m1 + 8.f);      // at most 256
+          const float2 f0 = ab[c], f1 = ab[c + 1];
+          l[c] = fmaf(w0 * back, f0.y, l[c] * f0.x);
+          l[c + 1] = fmaf(w1 * back, f1.y, l[c + 1] * f1.x);
+          // 11 bits, as three e4m3 values
+          __half2 r = __floats2half2_rn(w0, w1);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+            const uint32_t h = __nv_cvt_halfraw2_to_fp8x2((__half2_raw)r, __NV_SATFINITE, __NV_E4M3);
+            p_row[swz<AT_T>(p * C + c, tok)] = (uint8_t)h;
+            p_row[swz<AT_T>(p * C + c + 1, tok)] = (uint8_t)(h >> 8);
+            if (p < 2) r = __hmul2(__hsub2(r, __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h, __NV_E4M3))), __float2half2_rn(16.f));
+          }
+        }
+        // the values of a token that no column sees may be anything (its page may not even have been read): zeros
+        if ((t + 1) * AT_T > rp.c || masked) {
+          const int s = n % AT_RING;
+          if (!wait_all(sm.v_full[s], (uint32_t)(n / AT_RING))) break;
+          if (unseen) {
+            uint4 *z = reinterpret_cast<uint4 *>(base_ptr + (v_ring - base) + s * TILE + tok * HD);
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i) z[i] = make_uint4(0u, 0u, 0u, 0u);
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.p_ready[grp]));
+        ++k;
+      }
+      if (failed) break;
+      // the item's sums: over the lanes, then over the warps
+      const int ii = it - item_lo, h = ii & 1;
+      if (ii >= 2 && !wait_all(sm.l_free[h], (uint32_t)(ii / 2 - 1))) break;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float v = l[c];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0) sm.lpart[h][grp * 4 + wq][c] = v;
+      }
+      if (wq == 0 && lane < C) sm.lframe[h][grp][lane] = m_run;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.l_ready[h]));
+    }
+  } else {
+    // ---------------- output: thread = value dim, the running output of every column in registers ----------------
+    const int wq = warp & 3;
+    const bool has_dim = HD == 128 || lane < 16;
+    const int d = HD == 128 ? wq * 32 + lane : wq * 16 + lane;     // an M = 64 accumulator has 16 rows in each lane quarter
+    const uint32_t o_lane = o_tmem + ((uint32_t)(32 * wq) << 16);
+    float2 *ab = sm.ab[warp - 4];
+    float o[C];
+    int n = 0;
+    for (int it = item_lo; it < item_hi && !failed; ++it) {
+      const Item x = locate(it);
+      const int cols = x.ni * G;
+      float m_run = AT_LOW;                           // lane c: the running frame of column c
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = 0.f;
+      for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
+        const int h = n & 1;
+        if (!wait_all(sm.o_full[h], (uint32_t)(n / 2))) break;
+        tc_fence_after();
+        if (lane < C) {
+          const float m_tile = sm.frame[h][lane], m_new = fmaxf(m_run, m_tile);
+          ab[lane] = make_float2(ex2(m_run - m_new), ex2(m_tile - m_new));
+          m_run = m_new;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int c0 = 0; c0 < C; c0 += 8) {
+          constexpr int W = C < 8 ? C : 8;
+          uint32_t v[24];
+          if (C == 4) {
+            tmem_ld8(o_lane + (uint32_t)(h * N), *reinterpret_cast<uint32_t(*)[8]>(&v[0]));
+            tmem_ld8(o_lane + (uint32_t)(h * N + 8), *reinterpret_cast<uint32_t(*)[8]>(&v[8]));
+          } else {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) tmem_ld8(o_lane + (uint32_t)(h * N + p * C + c0), *reinterpret_cast<uint32_t(*)[8]>(&v[p * 8]));
+          }
+          tmem_ld_wait();
+#pragma unroll
+          for (int c = 0; c < W; ++c) {
+            const float f = fmaf(__uint_as_float(v[2 * W + c]), 1.f / 256.f, fmaf(__uint_as_float(v[W + c]), 1.f / 16.f, __uint_as_float(v[c])));
+            const float2 s = ab[c0 + c];
+            o[c0 + c] = fmaf(f, s.y, o[c0 + c] * s.x);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.o_free[h]));
+      }
+      if (failed) break;
+      const int ii = it - item_lo, h = ii & 1;
+      if (!wait_all(sm.l_ready[h], (uint32_t)(ii / 2))) break;
+      float L = 0.f;                                  // lane c: the sum of column c in the frame m_run
+      if (lane < C) {
+#pragma unroll
+        for (int gr = 0; gr < 2; ++gr) {
+          float v = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) v += sm.lpart[h][gr * 4 + w][lane];
+          L = fmaf(v, ex2(sm.lframe[h][gr][lane] - m_run), L);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.l_free[h]));
+      const long long bg = (long long)x.b * a.n_kv + x.g;
+      if (rp.ns == 1) {
+        const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const float f = __shfl_sync(0xffffffffu, inv, c);
+          if (c < cols && has_dim)
+            ((T *)a.out)[(long long)(rp.first + x.i0 + c / G) * a.o_t + (long long)(x.g * G + c % G) * a.o_h + d] = from_f32<T>(o[c] * f);
+        }
+        if (a.mass && wq == 0 && lane < cols) a.ml[bg * a.cols + lane] = make_float2(m_run - 8.f, inv);
+      } else {
+        const long long at = (bg * a.max_splits + x.split) * a.cols;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (c < cols && has_dim) a.part_o[(at + c) * HD + d] = o[c];
+        if (wq == 0 && lane < cols) a.part_ml[at + lane] = make_float2(m_run, L);
       }
     }
-    a.mass[(long long)blockIdx.x * reach + j] += sum;
+  }
+  if (failed || sm.abort_flag) {
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);   // let copies in flight land before the CTA retires
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (tid == 0)
+    for (int i = blockIdx.x; i < AT_STATUS; i += gridDim.x) a.status[i] = sm.abort_flag ? DEV_TIMEOUT_EPILOGUE : DEV_OK;
+  if (warp == 0) tmem_dealloc(s_tmem, TMEM_COLS);
+}
+
+// One block per (row, key head, column), one thread per dim: the row's splits in ascending order.
+template <typename T, int HD>
+__global__ void __launch_bounds__(HD) attend_combine_kernel(const __grid_constant__ AttendArgs a) {
+  griddep_launch_dependents();
+  __shared__ float2 sml[AT_SPLITS];
+  const int b = blockIdx.x / a.n_kv, g = blockIdx.x - b * a.n_kv, col = blockIdx.y, d = threadIdx.x, G = a.n_q / a.n_kv;
+  const int first = a.cu ? a.cu[b] : b, end = a.cu ? a.cu[b + 1] : b + 1;
+  const RowPlan r = row_plan(a.ctx[b], first, end, a, G, 1);       // (ns does not depend on the columns of a tile)
+  griddep_wait();
+  if (r.n == 0 || r.ns <= 1 || col >= r.n * G) return;
+  const long long at = (long long)blockIdx.x * a.max_splits;
+  for (int s = d; s < r.ns; s += HD) sml[s] = __ldcg(a.part_ml + (at + s) * a.cols + col);
+  __syncthreads();
+  float M = AT_LOW, L = 0.f, o = 0.f;
+  for (int s = 0; s < r.ns; ++s) M = fmaxf(M, sml[s].x);
+  const float *po = a.part_o + (at * a.cols + col) * HD + d;
+  const long long step = (long long)a.cols * HD;
+  for (int s0 = 0; s0 < r.ns; s0 += 8) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = s0 + e < r.ns ? __ldcg(po + (s0 + e) * step) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (s0 + e < r.ns) {
+        const float f = ex2(sml[s0 + e].x - M);
+        L = fmaf(f, sml[s0 + e].y, L);
+        o = fmaf(f, x[e], o);
+      }
+  }
+  const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
+  ((T *)a.out)[(long long)(first + col / G) * a.o_t + (long long)(g * G + col % G) * a.o_h + d] = from_f32<T>(o * inv);
+  if (a.mass && d == 0) a.ml[(long long)blockIdx.x * a.cols + col] = make_float2(M - 8.f, inv);
+}
+
+// One thread per cached token of a (row, key head): mass += the sum of its weights over the columns, ascending.
+__global__ void __launch_bounds__(256) attend_mass_kernel(const __grid_constant__ AttendArgs a) {
+  __shared__ float2 ml[AT_MAXC];
+  const int b = blockIdx.x / a.n_kv, G = a.n_q / a.n_kv;
+  const int first = a.cu ? a.cu[b] : b, end = a.cu ? a.cu[b + 1] : b + 1;
+  const RowPlan r = row_plan(a.ctx[b], first, end, a, G, 1);
+  griddep_wait();
+  if (r.n == 0) return;
+  const int cols = r.n * G;
+  if ((int)threadIdx.x < cols) ml[threadIdx.x] = __ldcg(a.ml + (long long)blockIdx.x * a.cols + threadIdx.x);
+  __syncthreads();
+  const float *sc = a.scores + (long long)blockIdx.x * a.score_tokens * a.cols;
+  float *mass = a.mass + (long long)blockIdx.x * a.max_blocks * a.block;
+  for (int j = r.t_lo * AT_T + blockIdx.y * 256 + threadIdx.x; j < r.c; j += gridDim.y * 256) {
+    float sum = 0.f;
+    for (int c = 0; c < cols; ++c) {
+      const float2 f = ml[c];
+      sum = fmaf(ex2(__ldcg(sc + (long long)j * a.cols + c) - f.x), f.y, sum);
+    }
+    mass[j] += sum;
   }
 }
 
-template <typename T, int HD>
-cudaError_t launch_attend(const AttendArgs &a, cudaStream_t st) {
-  cudaError_t ce = launch_k(attend_simple_kernel<T, HD>, dim3(a.T, (a.n_q + 3) / 4), dim3(128), 0, st, false, a);
-  if (ce == cudaSuccess && a.mass) ce = launch_k(attend_mass_simple_kernel<T, HD>, dim3(a.B * a.n_kv, 32), dim3(128), 0, st, false, a);
+constexpr int at_columns(int wanted) { return wanted <= 4 ? 4 : wanted <= 8 ? 8 : wanted <= 16 ? 16 : 32; }
+
+// Sizes of the workspace's parts, each on 256 bytes.
+struct AttendSpace {
+  int cols, max_splits;
+  int64_t part_ml, part_o, ml, scores, score_tokens, bytes;
+};
+AttendSpace attend_space(int64_t B, int max_new, int n_q, int n_kv, int hd, int block, int max_blocks, bool mass) {
+  auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+  const int64_t G = n_q / n_kv, all = G * max_new;
+  const int64_t reach_tiles = ((int64_t)max_blocks * block + AT_T - 1) / AT_T;
+  AttendSpace s;
+  s.cols = (int)(mass ? (all < AT_MAXC ? all : AT_MAXC) : (G > (all < AT_FEW ? all : AT_FEW) ? G : (all < AT_FEW ? all : AT_FEW)));
+  s.max_splits = (int)((reach_tiles + AT_MIN_TILES - 1) / AT_MIN_TILES);
+  if (s.max_splits > AT_SPLITS) s.max_splits = AT_SPLITS;
+  s.score_tokens = reach_tiles * AT_T;
+  s.part_ml = AT_STATUS * 4;
+  s.part_o = s.part_ml + up(B * n_kv * s.max_splits * s.cols * 8);
+  s.ml = s.part_o + up(s.max_splits > 1 ? B * n_kv * s.max_splits * s.cols * hd * 4 : 0);
+  s.scores = s.ml + up(mass ? B * n_kv * s.cols * 8 : 0);
+  s.bytes = s.scores + up(mass ? B * n_kv * s.score_tokens * s.cols * 4 : 0);
+  return s;
+}
+
+template <typename T, int HD, int C>
+cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev, int sms, cudaStream_t st) {
+  // the shared-memory size is opted into once per device
+  static std::atomic<uint64_t> done{0};
+  constexpr int smem = smem_bytes<HD, C>();
+  cudaError_t ce = cudaSuccess;
+  if (dev >= 64 || !(done.load() >> dev & 1)) {
+    ce = cudaFuncSetAttribute(attend_kernel<T, HD, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (ce != cudaSuccess) return ce;
+    if (dev < 64) done.fetch_or(1ull << dev);
+  }
+  ce = launch_k(attend_kernel<T, HD, C>, dim3(sms), dim3(AT_THREADS), smem, st, false, tm, a);
+  if (ce == cudaSuccess && a.max_splits > 1) {
+    const int G = a.n_q / a.n_kv, few = G * a.max_new < AT_FEW ? G * a.max_new : AT_FEW;
+    ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, G > few ? G : few), dim3(HD), 0, st, true, a);
+  }
+  if (ce == cudaSuccess && a.mass) {
+    int gy = (4 * sms + a.B * a.n_kv - 1) / (a.B * a.n_kv);
+    const long long most = (a.score_tokens + 255) / 256;
+    if (gy > most) gy = (int)most;
+    ce = launch_k(attend_mass_kernel, dim3(a.B * a.n_kv, gy), dim3(256), 0, st, true, a);
+  }
   return ce;
+}
+template <typename T, int HD>
+cudaError_t launch_attend(const CUtensorMap &tm, const AttendArgs &a, int dev, int sms, cudaStream_t st) {
+  const long long all = (long long)(a.n_q / a.n_kv) * a.max_new;
+  switch (at_columns(all > AT_MAXC ? AT_MAXC : (int)all)) {
+    case 4: return launch_attend_c<T, HD, 4>(tm, a, dev, sms, st);
+    case 8: return launch_attend_c<T, HD, 8>(tm, a, dev, sms, st);
+    case 16: return launch_attend_c<T, HD, 16>(tm, a, dev, sms, st);
+    default: return launch_attend_c<T, HD, 32>(tm, a, dev, sms, st);
+  }
 }
 
 }  // namespace
@@ -136,41 +810,47 @@ extern "C" {
 
 int64_t corun_kv8_attend_bytes(int32_t B, int32_t T, int32_t max_new, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t block,
                                int32_t max_blocks, int32_t with_mass) {
-  if (B < 1 || T < 1 || max_new < 1 || n_q < 1 || n_kv < 1 || head_dim < 1 || block < 1 || max_blocks < 1) return 0;
-  return 1024 + (int64_t)T * n_q * 8;
+  if (B < 1 || T < 1 || max_new < 1 || n_q < 1 || n_kv < 1 || n_q < n_kv || head_dim < 1 || block < 1 || max_blocks < 1) return 0;
+  return attend_space(B, max_new, n_q, n_kv, head_dim, block, max_blocks, with_mass != 0).bytes;
 }
 
 int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, int32_t max_new, const corun_heads *q,
                      const corun_heads *out, int32_t dtype, int32_t n_q, float scale, int32_t window, float *mass, void *ws,
                      int64_t ws_bytes, void *cuda_stream) {
   if (!kv8_cache_ok(cache) || !kv8_rows_ok(rows, cache) || !q || !out || !q->p || !out->p || (dtype != CORUN_BF16 && dtype != CORUN_F16) ||
-      rows->B > AT_MAXB || max_new < 1 || (!rows->cu && max_new != 1) || n_q < 1 || n_q % cache->n_kv || n_q / cache->n_kv > 32 || !(scale > 0.f) || isinf(scale) ||
-      window < 0 || (mass && (int64_t)max_new * (n_q / cache->n_kv) > 32) || !heads_on_16(*q, dtype) || !heads_on_16(*out, dtype) || !ws ||
+      rows->B > AT_MAXB || max_new < 1 || (!rows->cu && max_new != 1) || n_q < 1 || n_q % cache->n_kv || n_q / cache->n_kv > AT_MAXC || !(scale > 0.f) || isinf(scale) ||
+      window < 0 || (mass && (int64_t)max_new * (n_q / cache->n_kv) > AT_MAXC) || !heads_on_16(*q, dtype) || !heads_on_16(*out, dtype) || !ws ||
       !aligned_to(ws, 256))
     return CORUN_EINVAL;
   if (rows->T == 0) return CORUN_OK;
-  if (ws_bytes < corun_kv8_attend_bytes(rows->B, rows->T, max_new, n_q, cache->n_kv, cache->head_dim, cache->block, rows->max_blocks, mass != nullptr))
-    return CORUN_EINVAL;
+  const AttendSpace s = attend_space(rows->B, max_new, n_q, cache->n_kv, cache->head_dim, cache->block, rows->max_blocks, mass != nullptr);
+  if (ws_bytes < s.bytes) return CORUN_EINVAL;
+  int dev = 0, sms = 0;
+  cudaError_t ce = cudaGetDevice(&dev);
+  if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
+  CUtensorMap tm;
+  const int rc = tma_encode_u8_rows(&tm, cache->pool, (unsigned long long)cache->pages * 2 * cache->n_kv * cache->block, cache->head_dim, cache->block);
+  if (rc != CORUN_OK) return rc;
+  char *w = (char *)ws;
+  const AttendArgs a{cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new, window < (1 << 30) ? window : 0, s.cols, s.max_splits,
+                     rows->block_table, rows->ctx, rows->cu, q->p, out->p, q->token_stride, q->head_stride, out->token_stride, out->head_stride,
+                     scale * 1.4426950408889634f, mass, (int *)w, (float2 *)(w + s.part_ml), (float *)(w + s.part_o), (float2 *)(w + s.ml),
+                     (float *)(w + s.scores), s.score_tokens};
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  const AttendArgs a{(const uint8_t *)cache->pool, cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new,
-                     window, rows->block_table, rows->ctx, rows->cu, q->p, out->p, q->token_stride, q->head_stride, out->token_stride,
-                     out->head_stride, scale, mass, (float2 *)((char *)ws + 1024)};
-  cudaError_t ce = cudaMemsetAsync(ws, 0, 1024, st);
-  if (ce == cudaSuccess) {
-    if (dtype == CORUN_BF16) ce = cache->head_dim == 128 ? launch_attend<__nv_bfloat16, 128>(a, st) : launch_attend<__nv_bfloat16, 64>(a, st);
-    else ce = cache->head_dim == 128 ? launch_attend<__half, 128>(a, st) : launch_attend<__half, 64>(a, st);
-  }
+  if (dtype == CORUN_BF16) ce = cache->head_dim == 128 ? launch_attend<__nv_bfloat16, 128>(tm, a, dev, sms, st) : launch_attend<__nv_bfloat16, 64>(tm, a, dev, sms, st);
+  else ce = cache->head_dim == 128 ? launch_attend<__half, 128>(tm, a, dev, sms, st) : launch_attend<__half, 64>(tm, a, dev, sms, st);
   if (ce != cudaSuccess) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   return CORUN_OK;
 }
 
 int corun_kv8_sync(const void *ws, void *cuda_stream) {
   if (!ws) return CORUN_EINVAL;
-  int hs[256] = {0};
+  int hs[AT_STATUS] = {0};
   cudaError_t ce = cudaMemcpyAsync(hs, ws, sizeof(hs), cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream);
   if (ce == cudaSuccess) ce = cudaStreamSynchronize((cudaStream_t)cuda_stream);
   if (ce != cudaSuccess) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
-  for (int i = 0; i < 256; ++i)
+  for (int i = 0; i < AT_STATUS; ++i)
     if (hs[i]) return CORUN_ETIMEOUT;
   return CORUN_OK;
 }
