@@ -15,8 +15,8 @@
 // share in the result; the sum of weights takes w 2^-e_v back.
 // A tile's output stays in its own frame M; it is added to the running output, held in registers, in 32 bits.
 //
-// An item is (row, tile of query columns, key head, split).  Rows with one new token, or few (n G <= 16), are split into
-// at most AT_SPLITS parts of at least two tiles; rows with more are not.  The split depends on the row's own ctx, n and window alone, sums
+// An item is (row, tile of query columns, key head, split).  Rows with n G <= 32 columns are split into at most AT_SPLITS parts of at
+// least two tiles; rows with more are not.  The split depends on the row's own ctx, n and window alone, sums
 // have one fixed order, and which CTA computes an item has no influence on any value: a row's result does not depend on
 // the other rows.  Every CTA (one per SM) takes a stretch of the item list, cut by cost.
 //   warp 0        producer: block-table lookups, TMA loads, exponents
@@ -27,6 +27,7 @@
 // A second kernel combines a row's splits in ascending order, a third one adds up the weights from the scores that the
 // first wrote (4 bytes per token and column, where mass is wanted).  Every wait is bounded.
 #include <atomic>
+#include <type_traits>
 
 #include <math_constants.h>
 
@@ -39,9 +40,9 @@ constexpr int AT_MAXB = 1024;       // rows per call
 constexpr int AT_T = 128;           // tokens per tile
 constexpr int AT_SPLITS = 64;       // splits of a row at most
 constexpr int AT_MIN_TILES = 2;     // tiles of a split at least
-constexpr int AT_FEW = 16;          // columns up to which a row with several new tokens is split
-constexpr int AT_MAXC = 32;         // columns of a tile at most
+constexpr int AT_MAXC = 32;         // columns of a tile at most; rows with as many columns or fewer are split
 constexpr int AT_RING = 4;          // K tiles, and as many V tiles, in flight
+constexpr int AT_EXPS = 2 * AT_RING; // tiles whose exponents are held
 constexpr int AT_THREADS = 512;
 constexpr int AT_STATUS = 256;      // status words at the start of the workspace
 constexpr float AT_LOW = -1e30f;    // a maximum over nothing
@@ -79,7 +80,7 @@ __device__ __forceinline__ RowPlan row_plan(int c, int first, int end, const Att
   r.t_lo = a.window ? max(0, c - r.n - a.window + 1) / AT_T : 0;
   r.t_hi = at_ceil(c, AT_T);
   const int nt = r.t_hi - r.t_lo;
-  if (r.n == 1 || r.n * G <= AT_FEW) {
+  if ((long long)r.n * G <= AT_MAXC) {
     r.qt = 1;
     r.tps = max(AT_MIN_TILES, at_ceil(nt, AT_SPLITS));
     r.ns = at_ceil(nt, r.tps);
@@ -136,35 +137,43 @@ struct Item {
 template <int C>
 struct Smem {
   uint64_t k_full[AT_RING], k_empty[AT_RING], v_full[AT_RING], v_empty[AT_RING];
-  uint64_t q_ready, q_free, s_full[2], s_free[2], p_ready[2], p_free[2], o_full[2], o_free[2], e_full[2], e_free[2], x_bar[2], l_ready[2], l_free[2];
+  uint64_t q_ready[2], q_free[2], s_full[2], s_free[2], p_ready[2], p_free[2], o_full[2], o_free[2], e_full[AT_EXPS], x_bar[2], l_ready[2], l_free[2];
   uint32_t tmem;
   int abort_flag;
   int my_items[2];
   float q_mul[4][C];                 // 2^e of a query column times scale log2(e), by query tile
   float x_max[2][2][C][4];           // [group][use parity][column][warp]: maxima of 32 tokens
   float frame[2][C];                 // [tile parity]: the tile's frames
-  float2 ab[12][C];                  // [warp - 4]: factors of old and new of every column
+  float4 ab[12][C];                  // [warp - 4]: factors of old and new of every column, the tile's frame
   float lpart[2][8][C];              // [item parity][group * 4 + warp]: sums of weights
   float lframe[2][2][C];             // [item parity][group]: their frames
-  int8_t exps[2][2][8];              // [tile parity][kind][page of the tile]
+  int8_t exps[AT_EXPS][2][8];        // [tile][kind][page of the tile]
   int row_item[AT_MAXB + 1];         // first item of every row
   int row_ic[AT_MAXB + 1];           // cost of one of its items
+  int row_c[AT_MAXB], row_first[AT_MAXB], row_end[AT_MAXB];
   long long row_cost[AT_MAXB + 1];   // cost of the items before the row
 };
 
-template <int HD, int C>
-constexpr int smem_bytes() { return 2 * AT_RING * AT_T * HD + (C == 4 ? 16 : C == 8 ? 32 : 3 * C) * (HD + 2 * AT_T) + (int)sizeof(Smem<C>) + 2048; }
+// Columns of a product with `pieces` columns per query column: an M = 128 MMA takes N in steps of 16.
+__host__ __device__ constexpr int at_n(int pieces, int C) { return (pieces * C + 15) / 16 * 16; }
+// A bf16 query is two e4m3 values exactly (8 bits), an fp16 query three (11 bits).
+template <typename T> __host__ __device__ constexpr int q_pieces() { return std::is_same<T, __nv_bfloat16>::value ? 2 : 3; }
+template <typename T, int HD, int C>
+__host__ __device__ constexpr int q_bytes() { return (at_n(q_pieces<T>(), C) * HD + 1023) / 1024 * 1024; }
+template <typename T, int HD, int C>
+constexpr int smem_bytes() { return 2 * AT_RING * AT_T * HD + 2 * q_bytes<T, HD, C>() + 2 * at_n(3, C) * AT_T + (int)sizeof(Smem<C>) + 1024; }
 
 template <typename T, int HD, int C>
 __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ AttendArgs a) {
-  constexpr int N = C == 4 ? 16 : C == 8 ? 32 : 3 * C;          // an M = 128 MMA takes N in steps of 16
-  constexpr int TILE = AT_T * HD;
-  constexpr uint32_t TMEM_COLS = 4 * N <= 64 ? 64 : 4 * N <= 128 ? 128 : 4 * N <= 256 ? 256 : 512;
+  constexpr int QP = q_pieces<T>(), NQ = at_n(QP, C), N = at_n(3, C);   // columns of the scores and of the output
+  constexpr int TILE = AT_T * HD, Q_TILE = q_bytes<T, HD, C>();
+  constexpr int COLS = 2 * NQ + 2 * N;
+  constexpr uint32_t TMEM_COLS = COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t *base_ptr = smem_raw + (base - smem_u32(smem_raw));
-  // [K ring][V ring][query tile][two weight tiles][the rest]: tiles start on 1 KiB (the query tile's size is a multiple of it)
-  const uint32_t k_ring = base, v_ring = base + AT_RING * TILE, q_tile = base + 2 * AT_RING * TILE, p_tile = q_tile + (uint32_t)((N * HD + 1023) & ~1023);
+  // [K ring][V ring][two query tiles][two weight tiles][the rest], tiles on 1 KiB
+  const uint32_t k_ring = base, v_ring = base + AT_RING * TILE, q_tile = base + 2 * AT_RING * TILE, p_tile = q_tile + 2 * Q_TILE;
   uint8_t *q_ptr = base_ptr + (q_tile - base), *p_ptr = base_ptr + (p_tile - base);
   Smem<C> &sm = *reinterpret_cast<Smem<C> *>(p_ptr + 2 * N * AT_T);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -176,13 +185,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       mbar_init(smem_u32(&sm.k_full[s]), 1); mbar_init(smem_u32(&sm.k_empty[s]), 1);
       mbar_init(smem_u32(&sm.v_full[s]), 1); mbar_init(smem_u32(&sm.v_empty[s]), 1);
     }
-    mbar_init(smem_u32(&sm.q_ready), 2);
-    mbar_init(smem_u32(&sm.q_free), 1);
+    for (int s = 0; s < AT_EXPS; ++s) mbar_init(smem_u32(&sm.e_full[s]), 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&sm.s_full[s]), 1); mbar_init(smem_u32(&sm.s_free[s]), 4);
       mbar_init(smem_u32(&sm.p_ready[s]), 4); mbar_init(smem_u32(&sm.p_free[s]), 1);
       mbar_init(smem_u32(&sm.o_full[s]), 1); mbar_init(smem_u32(&sm.o_free[s]), 4);
-      mbar_init(smem_u32(&sm.e_full[s]), 1); mbar_init(smem_u32(&sm.e_free[s]), 4);
+      mbar_init(smem_u32(&sm.q_ready[s]), 2); mbar_init(smem_u32(&sm.q_free[s]), 1);
       mbar_init(smem_u32(&sm.x_bar[s]), 4);
       mbar_init(smem_u32(&sm.l_ready[s]), 8); mbar_init(smem_u32(&sm.l_free[s]), 4);
     }
@@ -208,7 +216,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       long long cst = 0;
       if (r < a.B) {
         const int first = a.cu ? __ldg(a.cu + r) : r, end = a.cu ? __ldg(a.cu + r + 1) : r + 1;
-        const RowPlan p = row_plan(__ldg(a.ctx + r), first, end, a, G, TQ);
+        const int ctx = __ldg(a.ctx + r);
+        const RowPlan p = row_plan(ctx, first, end, a, G, TQ);
+        sm.row_c[r] = ctx; sm.row_first[r] = first; sm.row_end[r] = end;
         n = p.qt * p.ns * a.n_kv;                     // 0 for a row that is left out
         // a tile's cost is 2, an item's beyond its tiles 1; with several query tiles the first see fewer tokens
         const int ic = 1 + 2 * (p.qt > 1 ? max(1, (p.c - p.n / 2) / AT_T + 1 - p.t_lo) : p.tps);
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t s_tmem = sm.tmem, o_tmem = s_tmem + 2 * N;
+  const uint32_t s_tmem = sm.tmem, o_tmem = s_tmem + 2 * NQ;
   const int item_lo = sm.my_items[0], item_hi = sm.my_items[1];
   bool failed = false;
   int cur = -1;
@@ -258,7 +268,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     bool moved = cur < 0;
     if (moved) cur = 0;
     while (it >= sm.row_item[cur + 1]) { ++cur; moved = true; }
-    if (moved) rp = row_plan(__ldg(a.ctx + cur), a.cu ? __ldg(a.cu + cur) : cur, a.cu ? __ldg(a.cu + cur + 1) : cur + 1, a, G, TQ);
+    if (moved) rp = row_plan(sm.row_c[cur], sm.row_first[cur], sm.row_end[cur], a, G, TQ);
     Item x;
     const int i = it - sm.row_item[cur], unit = i / rp.ns, qt = unit % rp.qt;
     x.b = cur;
@@ -285,54 +295,72 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
 
   if (warp == 0) {
     // ---------------- producer ----------------
+    // Tiles in batches of four, eight lanes a tile and a page a lane: while a batch is loaded, the exponents of the next
+    // one and the page numbers of the one after are on their way.
     const uint64_t pol = l2_policy_evict_normal();
-    const int per = AT_T / a.block;                   // pages of a tile: lane l looks after page l
-    int n = 0;
-    int it = item_lo, t = 0;
+    const int per = AT_T / a.block;                   // pages of a tile
+    const int y_none = (int)(a.pages * 2 * a.n_kv * a.block);          // behind the pool: a page outside of it reads as zeros
+    struct Batch { int cnt, np, g, page, ek, ev; };   // tiles; of the lane's tile: pages, key head; of its page: number, exponents
+    int it = item_lo, t = 0, n = 0;
     Item x = {};
-    // a cursor one tile ahead: its pages are looked up while the tile before is loaded
-    auto page_of = [&](const Item &y, int tile) {
-      const int j = tile * per + lane;
-      return lane < per && j * a.block < rp.c ? __ldg(a.block_table + (size_t)y.b * a.max_blocks + j) : -1;
-    };
-    int page = -1;
-    if (it < item_hi) { x = locate(it); t = x.t0; page = page_of(x, t); }
-    while (it < item_hi && !failed) {
-      // this tile
-      const int c = rp.c, g = x.g;
-      const int np = min(per, at_ceil(c - t * AT_T, a.block));
-      const bool page_ok = page >= 0 && (long long)page < a.pages;
-      const long long at = ((long long)page * 2) * a.n_kv + g;
-      int ek = 0, ev = 0;
-      if (lane < np && page_ok) { ek = __ldg(a.exps + at); ev = __ldg(a.exps + at + a.n_kv); }
-      const int y_none = (int)(a.pages * 2 * a.n_kv * a.block);       // behind the pool: a page outside of it reads as zeros
-      const int yk = page_ok ? (int)(at * a.block) : y_none, yv = page_ok ? (int)((at + a.n_kv) * a.block) : y_none;
-      // the next tile's pages
-      if (++t >= x.t1) {
-        if (++it < item_hi) { x = locate(it); t = x.t0; }
+    if (it < item_hi) { x = locate(it); t = x.t0; }
+    auto pages = [&](Batch &q) {
+      q.cnt = q.np = q.g = q.ek = q.ev = 0;
+      const int *src = nullptr;
+      for (; q.cnt < 4 && it < item_hi; ++q.cnt) {
+        if ((lane >> 3) == q.cnt) {
+          q.np = min(per, at_ceil(rp.c - t * AT_T, a.block));
+          q.g = x.g;
+          if ((lane & 7) < q.np) src = a.block_table + (size_t)x.b * a.max_blocks + (size_t)t * per + (lane & 7);
+        }
+        if (++t >= x.t1 && ++it < item_hi) { x = locate(it); t = x.t0; }
       }
-      page = it < item_hi ? page_of(x, t) : -1;
-      const int s = n % AT_RING;
-      const uint32_t bytes = (uint32_t)(np * a.block * HD);
-      if (n >= AT_RING && !wait_all(sm.k_empty[s], (uint32_t)(n / AT_RING - 1))) break;
-      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.k_full[s]), bytes);
-      __syncwarp();
-      if (lane < np) tma_load_2d(k_ring + (uint32_t)(s * TILE + lane * a.block * HD), &tm, 0, yk, smem_u32(&sm.k_full[s]), pol);
-      if (n >= AT_RING && !wait_all(sm.v_empty[s], (uint32_t)(n / AT_RING - 1))) break;
-      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.v_full[s]), bytes);
-      __syncwarp();
-      if (lane < np) tma_load_2d(v_ring + (uint32_t)(s * TILE + lane * a.block * HD), &tm, 0, yv, smem_u32(&sm.v_full[s]), pol);
-      if (n >= 2 && !wait_all(sm.e_free[n & 1], (uint32_t)(n / 2 - 1))) break;
-      if (lane < 8) { sm.exps[n & 1][0][lane] = (int8_t)ek; sm.exps[n & 1][1][lane] = (int8_t)ev; }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sm.e_full[n & 1]));
-      ++n;
+      q.page = src ? __ldg(src) : -1;
+    };
+    auto exponents = [&](Batch &q) {
+      if (q.page >= 0 && (long long)q.page < a.pages) {
+        const long long at = ((long long)q.page * 2) * a.n_kv + q.g;
+        q.ek = __ldg(a.exps + at);
+        q.ev = __ldg(a.exps + at + a.n_kv);
+      }
+    };
+    Batch b0, b1, b2;
+    pages(b0);
+    pages(b1);
+    exponents(b0);
+    while (b0.cnt > 0 && !failed) {
+      exponents(b1);
+      pages(b2);
+      const bool page_ok = b0.page >= 0 && (long long)b0.page < a.pages;
+      const long long at = ((long long)b0.page * 2) * a.n_kv + b0.g;
+      const int yk = page_ok ? (int)(at * a.block) : y_none, yv = page_ok ? (int)((at + a.n_kv) * a.block) : y_none;
+      for (int i = 0; i < b0.cnt; ++i, ++n) {
+        const int s = n % AT_RING;
+        const int np = __shfl_sync(0xffffffffu, b0.np, 8 * i);
+        const bool mine = (lane >> 3) == i && (lane & 7) < np;
+        const uint32_t bytes = (uint32_t)(np * a.block * HD), dst = (uint32_t)(s * TILE + (lane & 7) * a.block * HD);
+        if (n >= AT_RING && !wait_all(sm.k_empty[s], (uint32_t)(n / AT_RING - 1))) break;
+        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.k_full[s]), bytes);
+        __syncwarp();
+        if (mine) tma_load_2d(k_ring + dst, &tm, 0, yk, smem_u32(&sm.k_full[s]), pol);
+        if (n >= AT_RING && !wait_all(sm.v_empty[s], (uint32_t)(n / AT_RING - 1))) break;
+        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.v_full[s]), bytes);
+        __syncwarp();
+        if (mine) tma_load_2d(v_ring + dst, &tm, 0, yv, smem_u32(&sm.v_full[s]), pol);
+        // (the tile before the last AT_RING has been through its output product, so the exponents twice as far back have been read)
+        const int e = n % AT_EXPS;
+        if ((lane >> 3) == i) { sm.exps[e][0][lane & 7] = (int8_t)b0.ek; sm.exps[e][1][lane & 7] = (int8_t)b0.ev; }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.e_full[e]));
+      }
+      b0 = b1;
+      b1 = b2;
     }
   } else if (warp == 1) {
     // ---------------- MMA issuer ----------------
     if (elect_one()) {
       // D fp32, A and B e4m3 (format 0); scores: M = 128; output: M = hd, A MN-major
-      const uint32_t idesc_s = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(AT_T >> 4) << 24);
+      const uint32_t idesc_s = (1u << 4) | ((uint32_t)(NQ >> 3) << 17) | ((uint32_t)(AT_T >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 15) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(HD >> 4) << 24);
       auto wait = [&](uint64_t &bar, uint32_t parity) {
         if (!mbar_wait(smem_u32(&bar), parity & 1u, &sm.abort_flag)) failed = true;
@@ -359,10 +387,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       for (int it = item_lo; it < item_hi && !failed; ++it) {
         x = locate(it);
         if (it == item_lo || !same_query(x, last)) {
-          if (it > item_lo) umma_commit(smem_u32(&sm.q_free));        // every score product of the tile before has been issued
-          if (!wait(sm.q_ready, (uint32_t)n_q)) break;
+          if (n_q > 0) umma_commit(smem_u32(&sm.q_free[(n_q - 1) & 1]));   // every score product with the query tile before has been issued
+          if (!wait(sm.q_ready[n_q & 1], (uint32_t)(n_q / 2))) break;
           ++n_q;
         }
+        const uint32_t q_at = q_tile + (uint32_t)((n_q - 1) & 1) * Q_TILE;
         last = x;
         for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
           const int s = n % AT_RING, h = n & 1;
@@ -371,7 +400,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
           tc_fence_after();
 #pragma unroll
           for (int k = 0; k < HD / 32; ++k)
-            umma_f8(s_tmem + (uint32_t)(h * N), desc_hd<HD>(k_ring + (uint32_t)(s * TILE)) + (uint64_t)(k * 2), desc_hd<HD>(q_tile) + (uint64_t)(k * 2),
+            umma_f8(s_tmem + (uint32_t)(h * NQ), desc_hd<HD>(k_ring + (uint32_t)(s * TILE)) + (uint64_t)(k * 2), desc_hd<HD>(q_at) + (uint64_t)(k * 2),
                     idesc_s, k > 0 ? 1u : 0u);
           umma_commit(smem_u32(&sm.k_empty[s]));
           umma_commit(smem_u32(&sm.s_full[h]));
@@ -390,7 +419,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       x = locate(it);
       if (it > item_lo && same_query(x, last)) continue;
       last = x;
-      if (n_q > 0 && !wait_all(sm.q_free, (uint32_t)(n_q - 1))) break;
+      if (n_q > 1 && !wait_all(sm.q_free[n_q & 1], (uint32_t)(n_q / 2 - 1))) break;
+      uint8_t *q_at = q_ptr + (n_q & 1) * Q_TILE;
       const int cols = x.ni * G;
       for (int c = warp - 2; c < cols; c += 2) {
         const T *src = (const T *)a.q + (long long)(rp.first + x.i0 + c / G) * a.q_t + (long long)(x.g * G + c % G) * a.q_h + lane * EPL;
@@ -416,12 +446,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         // to [128, 256): e from the exponent bits (a subnormal maximum counts as 2^-126)
         const int e = max((__float_as_int(mx) >> 23) - 127, -110) - 7;
         const float down = pow2f(-e > 126 ? 126 : -e);
-        uint32_t w[3] = {0u, 0u, 0u};
+        uint32_t w[QP] = {};
 #pragma unroll
         for (int i = 0; i < EPL; i += 2) {
           float r0 = v[i] * down, r1 = v[i + 1] * down;
 #pragma unroll
-          for (int p = 0; p < 3; ++p) {
+          for (int p = 0; p < QP; ++p) {
             const uint32_t h = e4m3x2_of(r0, r1);
             const float2 f = e4m3x2_to(h);
             r0 = (r0 - f.x) * 16.f;
@@ -430,22 +460,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
           }
         }
 #pragma unroll
-        for (int p = 0; p < 3; ++p) {
-          uint8_t *dst = q_ptr + swz<HD>(p * C + c, lane * EPL);
+        for (int p = 0; p < QP; ++p) {
+          uint8_t *dst = q_at + swz<HD>(p * C + c, lane * EPL);
           if (EPL == 4) *reinterpret_cast<uint32_t *>(dst) = w[p]; else *reinterpret_cast<uint16_t *>(dst) = (uint16_t)w[p];
         }
         if (lane == 0) sm.q_mul[n_q & 3][c] = (mx > 0.f ? pow2f(e) : 1.f) * a.scale_log2e;
       }
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sm.q_ready));
+      if (lane == 0) mbar_arrive(smem_u32(&sm.q_ready[n_q & 1]));
       ++n_q;
     }
   } else if (warp < 12) {
     // ---------------- softmax: group 0 takes the even tiles, group 1 the odd ones ----------------
-    const int grp = warp >= 8 ? 1 : 0, wq = warp & 3, tok = wq * 32 + lane;
-    const uint32_t s_lane = s_tmem + ((uint32_t)(32 * wq) << 16) + (uint32_t)(grp * N);
-    float2 *ab = sm.ab[warp - 4];
+    const int grp = warp >= 8 ? 1 : 0, wq = warp & 3, tok = wq * 32 + lane, pg = tok / a.block;
+    const uint32_t s_lane = s_tmem + ((uint32_t)(32 * wq) << 16) + (uint32_t)(grp * NQ);
+    float4 *ab = sm.ab[warp - 4];
     float l[C];
     float m_run = AT_LOW;                             // lane c: the running frame of column c
     int n = 0, n_q = -1, k = 0;                       // k: tiles this group has done
@@ -462,13 +492,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
         if ((n & 1) != grp) continue;
         const int j = t * AT_T + tok;
-        if (!wait_all(sm.e_full[grp], (uint32_t)k)) break;
-        const int pg = tok / a.block;
-        const float ek = pow2f(sm.exps[grp][0][pg]);
-        const int ev_i = sm.exps[grp][1][pg];
+        if (!wait_all(sm.e_full[n % AT_EXPS], (uint32_t)(n / AT_EXPS))) break;
+        const float ek = pow2f(sm.exps[n % AT_EXPS][0][pg]);
+        const int ev_i = sm.exps[n % AT_EXPS][1][pg];
         const float ev = (float)ev_i;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sm.e_free[grp]));
         if (!wait_all(sm.s_full[grp], (uint32_t)k)) break;
         tc_fence_after();
         const bool masked = (t + 1) * AT_T > lim0 + 1 || (a.window && t * AT_T <= lim1 - a.window);
@@ -478,22 +505,24 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         bool unseen = true;                           // no column sees the token
 #pragma unroll
         for (int c0 = 0; c0 < C; c0 += 16) {
-          uint32_t v[3 * (C < 16 ? C : 16)];
-          constexpr int W = C < 16 ? C : 16;
+          constexpr int W = C < 16 ? C : 16, LD = C == 4 ? 16 : QP * W;
+          uint32_t v[LD];
           if (C == 4) {
             tmem_ld8(s_lane, *reinterpret_cast<uint32_t(*)[8]>(&v[0]));
-            asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]) : "r"(s_lane + 8) : "memory");
+            if (QP == 3) tmem_ld8(s_lane + 8, *reinterpret_cast<uint32_t(*)[8]>(&v[8]));
           } else if (C == 8) {
 #pragma unroll
-            for (int p = 0; p < 3; ++p) tmem_ld8(s_lane + (uint32_t)(p * C), *reinterpret_cast<uint32_t(*)[8]>(&v[p * W]));
+            for (int p = 0; p < QP; ++p) tmem_ld8(s_lane + (uint32_t)(p * C), *reinterpret_cast<uint32_t(*)[8]>(&v[p * W]));
           } else {
 #pragma unroll
-            for (int p = 0; p < 3; ++p) tmem_ld16(s_lane + (uint32_t)(p * C + c0), *reinterpret_cast<uint32_t(*)[16]>(&v[(p * W) % (3 * W)]));
+            for (int p = 0; p < QP; ++p) tmem_ld16(s_lane + (uint32_t)(p * C + c0), *reinterpret_cast<uint32_t(*)[16]>(&v[(p * W) % LD]));
           }
           tmem_ld_wait();
 #pragma unroll
           for (int c = 0; c < W; ++c) {
-            const float s = fmaf(__uint_as_float(v[2 * W + c]), 1.f / 256.f, fmaf(__uint_as_float(v[W + c]), 1.f / 16.f, __uint_as_float(v[c])));
+            float s = __uint_as_float(v[(QP - 1) * W + c]);
+#pragma unroll
+            for (int p = QP - 2; p >= 0; --p) s = fmaf(s, 1.f / 16.f, __uint_as_float(v[p * W + c]));
             y[c0 + c] = s * (ek * qm[c0 + c]);
           }
         }
@@ -534,7 +563,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
           const float4 f = *reinterpret_cast<const float4 *>(xm[lane]);
           m_tile = fmaxf(fmaxf(fmaxf(f.x, f.y), fmaxf(f.z, f.w)), AT_LOW);
           const float m_new = fmaxf(m_run, m_tile);
-          ab[lane] = make_float2(ex2(m_run - m_new), ex2(m_tile - m_new));
+          ab[lane] = make_float4(ex2(m_run - m_new), ex2(m_tile - m_new), m_tile - 8.f, 0.f);
           m_run = m_new;
         }
         // P of the tile before the last must have been read, and its frames
@@ -544,12 +573,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         __syncwarp();
         uint8_t *p_row = p_ptr + grp * N * AT_T;
         const float back = pow2f(-ev_i);
-        float m_all = m_tile;
 #pragma unroll
         for (int c = 0; c < C; c += 2) {
-          const float m0 = __shfl_sync(0xffffffffu, m_all, c), m1 = __shfl_sync(0xffffffffu, m_all, c + 1);
-          const float w0 = ex2(y[c] - m0 + 8.f), w1 = ex2(y[c + 1] - m1 + 8.f);      // at most 256
-          const float2 f0 = ab[c], f1 = ab[c + 1];
+          const float4 f0 = ab[c], f1 = ab[c + 1];
+          const float w0 = ex2(y[c] - f0.z), w1 = ex2(y[c + 1] - f1.z);              // at most 256
           l[c] = fmaf(w0 * back, f0.y, l[c] * f0.x);
           l[c + 1] = fmaf(w1 * back, f1.y, l[c + 1] * f1.x);
           // 11 bits, as three e4m3 values
@@ -598,7 +625,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     const bool has_dim = HD == 128 || lane < 16;
     const int d = HD == 128 ? wq * 32 + lane : wq * 16 + lane;     // an M = 64 accumulator has 16 rows in each lane quarter
     const uint32_t o_lane = o_tmem + ((uint32_t)(32 * wq) << 16);
-    float2 *ab = sm.ab[warp - 4];
+    float4 *ab = sm.ab[warp - 4];
     float o[C];
     int n = 0;
     for (int it = item_lo; it < item_hi && !failed; ++it) {
@@ -613,7 +640,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         tc_fence_after();
         if (lane < C) {
           const float m_tile = sm.frame[h][lane], m_new = fmaxf(m_run, m_tile);
-          ab[lane] = make_float2(ex2(m_run - m_new), ex2(m_tile - m_new));
+          ab[lane] = make_float4(ex2(m_run - m_new), ex2(m_tile - m_new), 0.f, 0.f);
           m_run = m_new;
         }
         __syncwarp();
@@ -631,8 +658,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
           tmem_ld_wait();
 #pragma unroll
           for (int c = 0; c < W; ++c) {
-            const float f = fmaf(__uint_as_float(v[2 * W + c]), 1.f / 256.f, fmaf(__uint_as_float(v[W + c]), 1.f / 16.f, __uint_as_float(v[c])));
-            const float2 s = ab[c0 + c];
+            const float f = fmaf(fmaf(__uint_as_float(v[2 * W + c]), 1.f / 16.f, __uint_as_float(v[W + c])), 1.f / 16.f, __uint_as_float(v[c]));
+            const float4 s = ab[c0 + c];
             o[c0 + c] = fmaf(f, s.y, o[c0 + c] * s.x);
           }
         }
@@ -754,7 +781,7 @@ AttendSpace attend_space(int64_t B, int max_new, int n_q, int n_kv, int hd, int 
   const int64_t G = n_q / n_kv, all = G * max_new;
   const int64_t reach_tiles = ((int64_t)max_blocks * block + AT_T - 1) / AT_T;
   AttendSpace s;
-  s.cols = (int)(mass ? (all < AT_MAXC ? all : AT_MAXC) : (G > (all < AT_FEW ? all : AT_FEW) ? G : (all < AT_FEW ? all : AT_FEW)));
+  s.cols = (int)(all < AT_MAXC ? all : AT_MAXC);
   s.max_splits = (int)((reach_tiles + AT_MIN_TILES - 1) / AT_MIN_TILES);
   if (s.max_splits > AT_SPLITS) s.max_splits = AT_SPLITS;
   s.score_tokens = reach_tiles * AT_T;
@@ -770,7 +797,7 @@ template <typename T, int HD, int C>
 cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev, int sms, cudaStream_t st) {
   // the shared-memory size is opted into once per device
   static std::atomic<uint64_t> done{0};
-  constexpr int smem = smem_bytes<HD, C>();
+  constexpr int smem = smem_bytes<T, HD, C>();
   cudaError_t ce = cudaSuccess;
   if (dev >= 64 || !(done.load() >> dev & 1)) {
     ce = cudaFuncSetAttribute(attend_kernel<T, HD, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -779,8 +806,7 @@ cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev,
   }
   ce = launch_k(attend_kernel<T, HD, C>, dim3(sms), dim3(AT_THREADS), smem, st, false, tm, a);
   if (ce == cudaSuccess && a.max_splits > 1) {
-    const int G = a.n_q / a.n_kv, few = G * a.max_new < AT_FEW ? G * a.max_new : AT_FEW;
-    ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, G > few ? G : few), dim3(HD), 0, st, true, a);
+    ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, a.cols), dim3(HD), 0, st, true, a);
   }
   if (ce == cudaSuccess && a.mass) {
     int gy = (4 * sms + a.B * a.n_kv - 1) / (a.B * a.n_kv);
