@@ -41,8 +41,8 @@ constexpr int AT_T = 128;           // tokens per tile
 constexpr int AT_SPLITS = 64;       // splits of a row at most
 constexpr int AT_MIN_TILES = 2;     // tiles of a split at least
 constexpr int AT_MAXC = 32;         // columns of a tile at most; rows with as many columns or fewer are split
-constexpr int AT_RING = 4;          // K tiles, and as many V tiles, in flight
-constexpr int AT_EXPS = 2 * AT_RING; // tiles whose exponents are held
+// Tiles (keys and values) in shared memory: as many as fit beside the columns' operands.
+__host__ __device__ constexpr int at_ring(int C) { return C > 16 ? 4 : 5; }
 constexpr int AT_THREADS = 512;
 constexpr int AT_STATUS = 256;      // status words at the start of the workspace
 constexpr float AT_LOW = -1e30f;    // a maximum over nothing
@@ -65,33 +65,38 @@ struct AttendArgs {
   long long score_tokens;
 };
 
-// What a row asks for: its new tokens (0 = left out), the tiles it reads, its splits.
+// What a row asks for: its new tokens (0 = left out), the tiles it reads, its splits of tps tiles (0 = not this kernel's).
 struct RowPlan {
-  int c, n, first, t_lo, t_hi, ns, tps, qt;   // ns splits of tps tiles; qt query tiles
+  int c, n, first, t_lo, t_hi, ns, tps;
 };
-__host__ __device__ inline int at_ceil(int a, int b) { return (a + b - 1) / b; }
-__device__ __forceinline__ RowPlan row_plan(int c, int first, int end, const AttendArgs &a, int G, int TQ) {
+__device__ __forceinline__ int at_tps(int tiles) { return max(AT_MIN_TILES, (tiles + AT_SPLITS - 1) / AT_SPLITS); }
+__device__ __forceinline__ int at_lo(int c, int n, int window) { return window ? max(0, c - n - window + 1) / AT_T : 0; }
+__device__ __forceinline__ RowPlan row_plan(int c, int first, int end, const AttendArgs &a, int G) {
   RowPlan r;
   r.c = c;
   r.first = first;
   r.n = end - first;
   const bool ok = c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && r.n > 0 && r.n <= a.max_new && end <= a.T;
-  if (!ok) { r.n = 0; r.ns = 0; r.qt = 0; r.t_lo = r.t_hi = 0; r.tps = 1; return r; }
-  r.t_lo = a.window ? max(0, c - r.n - a.window + 1) / AT_T : 0;
-  r.t_hi = at_ceil(c, AT_T);
+  if (!ok) { r.n = 0; r.ns = 0; r.t_lo = r.t_hi = 0; r.tps = 1; return r; }
+  r.t_lo = at_lo(c, r.n, a.window);
+  r.t_hi = (c + AT_T - 1) / AT_T;
   const int nt = r.t_hi - r.t_lo;
-  if ((long long)r.n * G <= AT_MAXC) {
-    r.qt = 1;
-    r.tps = max(AT_MIN_TILES, at_ceil(nt, AT_SPLITS));
-    r.ns = at_ceil(nt, r.tps);
-  } else {
-    r.qt = at_ceil(r.n, TQ);
-    r.tps = nt;
-    r.ns = 1;
-  }
+  r.tps = at_tps(nt);
+  r.ns = (long long)r.n * G <= AT_MAXC ? (nt + r.tps - 1) / r.tps : 0;
   return r;
 }
 
+// Loads that are issued where they stand (the compiler may move an ordinary one down to its first use).
+__device__ __forceinline__ int load_now(const int *p) {
+  int v;
+  asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ int load_now(const int8_t *p) {
+  int v;
+  asm volatile("ld.global.nc.s8 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -110,34 +115,30 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Rows of 64 bytes with the 64-byte swizzle: groups of eight rows are 512 bytes; layout type 4.  K-major and, with one
-// block of 64 M elements, MN-major tiles alike (the stride byte offset is the distance of groups of eight rows in both).
-__device__ __forceinline__ uint64_t desc_sw64(uint32_t smem_addr) {
+// Descriptor of a tile whose rows of W bytes (128 or 64, swizzled by that width) come in groups of eight, `group` bytes
+// apart.  It serves K-major operands (rows = M or N) and, with W values of the M index in a row, MN-major ones (rows = K) alike: the
+// stride byte offset is the distance of the groups in both.
+template <int W>
+__device__ __forceinline__ uint64_t desc_rows(uint32_t smem_addr, uint32_t group) {
   uint64_t d = 0;
   d |= (uint64_t)((smem_addr >> 4) & 0x3FFFu);
   d |= (uint64_t)1u << 16;
-  d |= (uint64_t)(512u >> 4) << 32;
+  d |= (uint64_t)(group >> 4) << 32;
   d |= (uint64_t)1u << 46;
-  d |= (uint64_t)4u << 61;
+  d |= (uint64_t)(W == 128 ? 2u : 4u) << 61;
   return d;
 }
-template <int HD>
-__device__ __forceinline__ uint64_t desc_hd(uint32_t smem_addr) { return HD == 128 ? umma_desc_sw128(smem_addr) : desc_sw64(smem_addr); }
 // Byte b of row r of a swizzled tile with rows of W bytes (128: chunk ^ row mod 8, 64: chunk ^ row / 2 mod 4).
 template <int W>
 __device__ __forceinline__ uint32_t swz(int r, int b) {
   return W == 128 ? (uint32_t)(r * 128 + ((((b >> 4) ^ (r & 7)) << 4) | (b & 15))) : (uint32_t)(r * 64 + ((((b >> 4) ^ ((r >> 1) & 3)) << 4) | (b & 15)));
 }
 
-// An item of the list.
-struct Item {
-  int b, g, split, i0, ni, t0, t1;   // row, key head, split, first query token of the tile, their number, tiles [t0, t1)
-};
-
 template <int C>
 struct Smem {
-  uint64_t k_full[AT_RING], k_empty[AT_RING], v_full[AT_RING], v_empty[AT_RING];
-  uint64_t q_ready[2], q_free[2], s_full[2], s_free[2], p_ready[2], p_free[2], o_full[2], o_free[2], e_full[AT_EXPS], x_bar[2], l_ready[2], l_free[2];
+  static constexpr int RING = at_ring(C), EXPS = 2 * RING;         // EXPS: tiles whose exponents are held
+  uint64_t full[RING], empty[RING], e_full[EXPS];
+  uint64_t q_ready[2], q_free[2], s_full[2], s_free[2], p_ready[2], p_free[2], o_full[2], o_free[2], x_bar[2], l_ready[2], l_free[2];
   uint32_t tmem;
   int abort_flag;
   int my_items[2];
@@ -147,10 +148,10 @@ struct Smem {
   float4 ab[12][C];                  // [warp - 4]: factors of old and new of every column, the tile's frame
   float lpart[2][8][C];              // [item parity][group * 4 + warp]: sums of weights
   float lframe[2][2][C];             // [item parity][group]: their frames
-  int8_t exps[AT_EXPS][2][8];        // [tile][kind][page of the tile]
+  int8_t exps[EXPS][2][8];           // [tile][kind][page of the tile]
   int row_item[AT_MAXB + 1];         // first item of every row
   int row_ic[AT_MAXB + 1];           // cost of one of its items
-  int row_c[AT_MAXB], row_first[AT_MAXB], row_end[AT_MAXB];
+  int row_c[AT_MAXB], row_first[AT_MAXB], row_n[AT_MAXB];
   long long row_cost[AT_MAXB + 1];   // cost of the items before the row
 };
 
@@ -161,31 +162,30 @@ template <typename T> __host__ __device__ constexpr int q_pieces() { return std:
 template <typename T, int HD, int C>
 __host__ __device__ constexpr int q_bytes() { return (at_n(q_pieces<T>(), C) * HD + 1023) / 1024 * 1024; }
 template <typename T, int HD, int C>
-constexpr int smem_bytes() { return 2 * AT_RING * AT_T * HD + 2 * q_bytes<T, HD, C>() + 2 * at_n(3, C) * AT_T + (int)sizeof(Smem<C>) + 1024; }
+constexpr int smem_bytes() { return 2 * at_ring(C) * AT_T * HD + 2 * q_bytes<T, HD, C>() + 2 * at_n(3, C) * AT_T + (int)sizeof(Smem<C>) + 1024; }
 
 template <typename T, int HD, int C>
 __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ AttendArgs a) {
   constexpr int QP = q_pieces<T>(), NQ = at_n(QP, C), N = at_n(3, C);   // columns of the scores and of the output
-  constexpr int TILE = AT_T * HD, Q_TILE = q_bytes<T, HD, C>();
+  constexpr int RING = at_ring(C), EXPS = 2 * RING, GROUP = 8 * HD, TILE = 2 * AT_T * HD, Q_TILE = q_bytes<T, HD, C>();
   constexpr int COLS = 2 * NQ + 2 * N;
   constexpr uint32_t TMEM_COLS = COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t *base_ptr = smem_raw + (base - smem_u32(smem_raw));
-  // [K ring][V ring][two query tiles][two weight tiles][the rest], tiles on 1 KiB
-  const uint32_t k_ring = base, v_ring = base + AT_RING * TILE, q_tile = base + 2 * AT_RING * TILE, p_tile = q_tile + 2 * Q_TILE;
+  // [ring of tiles][two query tiles][two weight tiles][the rest], tiles on 1 KiB.  A tile of 128 tokens: eight rows of keys, eight
+  // rows of values, the next eight of keys, ...: a page's keys and values come with one box, and the groups of either are at
+  // one distance throughout (the TMA instruction takes some 70 cycles to issue: the fewer boxes the better)
+  const uint32_t ring = base, q_tile = base + RING * TILE, p_tile = q_tile + 2 * Q_TILE;
   uint8_t *q_ptr = base_ptr + (q_tile - base), *p_ptr = base_ptr + (p_tile - base);
   Smem<C> &sm = *reinterpret_cast<Smem<C> *>(p_ptr + 2 * N * AT_T);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int G = a.n_q / a.n_kv, TQ = C / G;
+  const int G = a.n_q / a.n_kv, shift = a.block == 16 ? 4 : a.block == 32 ? 5 : 6;
 
   if (tid == 0) {
     sm.abort_flag = 0;
-    for (int s = 0; s < AT_RING; ++s) {
-      mbar_init(smem_u32(&sm.k_full[s]), 1); mbar_init(smem_u32(&sm.k_empty[s]), 1);
-      mbar_init(smem_u32(&sm.v_full[s]), 1); mbar_init(smem_u32(&sm.v_empty[s]), 1);
-    }
-    for (int s = 0; s < AT_EXPS; ++s) mbar_init(smem_u32(&sm.e_full[s]), 1);
+    for (int s = 0; s < RING; ++s) { mbar_init(smem_u32(&sm.full[s]), 1); mbar_init(smem_u32(&sm.empty[s]), 1); }
+    for (int s = 0; s < EXPS; ++s) mbar_init(smem_u32(&sm.e_full[s]), 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&sm.s_full[s]), 1); mbar_init(smem_u32(&sm.s_free[s]), 4);
       mbar_init(smem_u32(&sm.p_ready[s]), 4); mbar_init(smem_u32(&sm.p_free[s]), 1);
@@ -217,11 +217,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       if (r < a.B) {
         const int first = a.cu ? __ldg(a.cu + r) : r, end = a.cu ? __ldg(a.cu + r + 1) : r + 1;
         const int ctx = __ldg(a.ctx + r);
-        const RowPlan p = row_plan(ctx, first, end, a, G, TQ);
-        sm.row_c[r] = ctx; sm.row_first[r] = first; sm.row_end[r] = end;
-        n = p.qt * p.ns * a.n_kv;                     // 0 for a row that is left out
-        // a tile's cost is 2, an item's beyond its tiles 1; with several query tiles the first see fewer tokens
-        const int ic = 1 + 2 * (p.qt > 1 ? max(1, (p.c - p.n / 2) / AT_T + 1 - p.t_lo) : p.tps);
+        const RowPlan p = row_plan(ctx, first, end, a, G);
+        sm.row_c[r] = ctx; sm.row_first[r] = first; sm.row_n[r] = p.n;
+        n = p.ns * a.n_kv;                            // 0 for a row that is left out
+        const int ic = 1 + 2 * p.tps;                 // a tile's cost is 2, an item's beyond its tiles 1
         sm.row_ic[r] = ic;
         cst = (long long)n * ic;
       }
@@ -262,31 +261,51 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
   const uint32_t s_tmem = sm.tmem, o_tmem = s_tmem + 2 * NQ;
   const int item_lo = sm.my_items[0], item_hi = sm.my_items[1];
   bool failed = false;
-  int cur = -1;
-  RowPlan rp = {};
-  auto locate = [&](int it) {                         // items ascend: the row pointer only moves forward
-    bool moved = cur < 0;
-    if (moved) cur = 0;
-    while (it >= sm.row_item[cur + 1]) { ++cur; moved = true; }
-    if (moved) rp = row_plan(sm.row_c[cur], sm.row_first[cur], sm.row_end[cur], a, G, TQ);
-    Item x;
-    const int i = it - sm.row_item[cur], unit = i / rp.ns, qt = unit % rp.qt;
-    x.b = cur;
-    x.split = i - unit * rp.ns;
-    x.g = unit / rp.qt;
-    x.i0 = qt * TQ;
-    x.ni = min(TQ, rp.n - x.i0);
-    if (rp.qt > 1 || rp.ns == 1) {                    // whole range of the tile's own queries
-      const int lim0 = rp.c - rp.n + x.i0, lim1 = lim0 + x.ni - 1;
-      x.t0 = a.window ? max(0, lim0 - a.window + 1) / AT_T : 0;
-      x.t1 = max(x.t0 + 1, lim1 < 0 ? 0 : lim1 / AT_T + 1);
-    } else {
-      x.t0 = rp.t_lo + x.split * rp.tps;
-      x.t1 = min(rp.t_hi, x.t0 + rp.tps);
-    }
-    return x;
+  // Where a role is in the CTA's stretch: the item (row b, key head g, split) and its tiles [t0, t1).  Going on to the next item takes
+  // additions only (a division here would cost every role some hundred cycles an item).
+  struct Cursor { int it, b, g, split, ns, tps, c, n, first, t_lo, t_hi, t0, t1; bool new_query; } x = {};
+  auto row_at = [&]() {
+    x.c = sm.row_c[x.b]; x.n = sm.row_n[x.b]; x.first = sm.row_first[x.b];
+    x.t_lo = at_lo(x.c, x.n, a.window);
+    x.t_hi = (x.c + AT_T - 1) / AT_T;
+    x.tps = at_tps(x.t_hi - x.t_lo);
   };
-  auto same_query = [](const Item &x, const Item &y) { return x.b == y.b && x.g == y.g && x.i0 == y.i0; };
+  auto tiles_at = [&]() {
+    x.t0 = x.t_lo + x.split * x.tps;
+    x.t1 = min(x.t_hi, x.t0 + x.tps);
+  };
+  x.it = item_lo;
+  x.new_query = true;
+  if (item_lo < item_hi) {
+    int lo = 0, hi = a.B;
+    while (hi - lo > 1) {                             // the row whose items hold item_lo (rows without items do not)
+      const int mid = (lo + hi) >> 1;
+      if (sm.row_item[mid] <= item_lo) lo = mid; else hi = mid;
+    }
+    x.b = lo;
+    row_at();
+    x.ns = (sm.row_item[lo + 1] - sm.row_item[lo]) / a.n_kv;
+    x.g = (item_lo - sm.row_item[lo]) / x.ns;
+    x.split = item_lo - sm.row_item[lo] - x.g * x.ns;
+    tiles_at();
+  }
+  auto next_item = [&]() {
+    ++x.it;
+    x.new_query = false;
+    if (++x.split == x.ns) {
+      x.split = 0;
+      x.new_query = true;
+      if (++x.g == a.n_kv) {
+        x.g = 0;
+        if (x.it < item_hi) {
+          do ++x.b; while (sm.row_item[x.b + 1] == x.it);
+          row_at();
+          x.ns = (x.t_hi - x.t_lo + x.tps - 1) / x.tps;
+        }
+      }
+    }
+    tiles_at();
+  };
   auto wait_all = [&](uint64_t &bar, uint32_t parity) {   // by a whole warp
     const bool ok = mbar_wait(smem_u32(&bar), parity & 1u, &sm.abort_flag);
     if (!__all_sync(0xffffffffu, ok)) failed = true;
@@ -298,30 +317,28 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     // Tiles in batches of four, eight lanes a tile and a page a lane: while a batch is loaded, the exponents of the next
     // one and the page numbers of the one after are on their way.
     const uint64_t pol = l2_policy_evict_normal();
-    const int per = AT_T / a.block;                   // pages of a tile
-    const int y_none = (int)(a.pages * 2 * a.n_kv * a.block);          // behind the pool: a page outside of it reads as zeros
+    const int per = AT_T >> shift;                   // pages of a tile
     struct Batch { int cnt, np, g, page, ek, ev; };   // tiles; of the lane's tile: pages, key head; of its page: number, exponents
-    int it = item_lo, t = 0, n = 0;
-    Item x = {};
-    if (it < item_hi) { x = locate(it); t = x.t0; }
+    int t = x.t0, n = 0;
     auto pages = [&](Batch &q) {
       q.cnt = q.np = q.g = q.ek = q.ev = 0;
       const int *src = nullptr;
-      for (; q.cnt < 4 && it < item_hi; ++q.cnt) {
+      for (; q.cnt < 4 && x.it < item_hi; ++q.cnt) {
         if ((lane >> 3) == q.cnt) {
-          q.np = min(per, at_ceil(rp.c - t * AT_T, a.block));
+          q.np = min(per, (x.c - t * AT_T + a.block - 1) >> shift);
           q.g = x.g;
           if ((lane & 7) < q.np) src = a.block_table + (size_t)x.b * a.max_blocks + (size_t)t * per + (lane & 7);
         }
-        if (++t >= x.t1 && ++it < item_hi) { x = locate(it); t = x.t0; }
+        if (++t >= x.t1) { next_item(); t = x.t0; }
       }
-      q.page = src ? __ldg(src) : -1;
+      q.page = -1;
+      if (src) q.page = load_now(src);
     };
     auto exponents = [&](Batch &q) {
       if (q.page >= 0 && (long long)q.page < a.pages) {
         const long long at = ((long long)q.page * 2) * a.n_kv + q.g;
-        q.ek = __ldg(a.exps + at);
-        q.ev = __ldg(a.exps + at + a.n_kv);
+        q.ek = load_now(a.exps + at);
+        q.ev = load_now(a.exps + at + a.n_kv);
       }
     };
     Batch b0, b1, b2;
@@ -332,23 +349,18 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       exponents(b1);
       pages(b2);
       const bool page_ok = b0.page >= 0 && (long long)b0.page < a.pages;
-      const long long at = ((long long)b0.page * 2) * a.n_kv + b0.g;
-      const int yk = page_ok ? (int)(at * a.block) : y_none, yv = page_ok ? (int)((at + a.n_kv) * a.block) : y_none;
+      const int page = page_ok ? b0.page : (int)a.pages;               // behind the pool: a page outside of it reads as zeros
+      const int group = b0.g * (a.block >> 3);
       for (int i = 0; i < b0.cnt; ++i, ++n) {
-        const int s = n % AT_RING;
+        const int s = n % RING;
         const int np = __shfl_sync(0xffffffffu, b0.np, 8 * i);
-        const bool mine = (lane >> 3) == i && (lane & 7) < np;
-        const uint32_t bytes = (uint32_t)(np * a.block * HD), dst = (uint32_t)(s * TILE + (lane & 7) * a.block * HD);
-        if (n >= AT_RING && !wait_all(sm.k_empty[s], (uint32_t)(n / AT_RING - 1))) break;
-        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.k_full[s]), bytes);
+        if (n >= RING && !wait_all(sm.empty[s], (uint32_t)(n / RING - 1))) break;
+        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.full[s]), (uint32_t)(np * a.block * 2 * HD));
         __syncwarp();
-        if (mine) tma_load_2d(k_ring + dst, &tm, 0, yk, smem_u32(&sm.k_full[s]), pol);
-        if (n >= AT_RING && !wait_all(sm.v_empty[s], (uint32_t)(n / AT_RING - 1))) break;
-        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.v_full[s]), bytes);
-        __syncwarp();
-        if (mine) tma_load_2d(v_ring + dst, &tm, 0, yv, smem_u32(&sm.v_full[s]), pol);
-        // (the tile before the last AT_RING has been through its output product, so the exponents twice as far back have been read)
-        const int e = n % AT_EXPS;
+        if ((lane >> 3) == i && (lane & 7) < np)
+          tma_load_5d(ring + (uint32_t)(s * TILE + (lane & 7) * a.block * 2 * HD), &tm, 0, 0, 0, group, page, smem_u32(&sm.full[s]), pol);
+        // (the tile RING before this one has been through its output product, so the exponents twice as far back have been read)
+        const int e = n % EXPS;
         if ((lane >> 3) == i) { sm.exps[e][0][lane & 7] = (int8_t)b0.ek; sm.exps[e][1][lane & 7] = (int8_t)b0.ev; }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.e_full[e]));
@@ -367,42 +379,38 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         return !failed;
       };
       auto output = [&](int n) {                      // the product of tile n's weights and values
-        const int s = n % AT_RING, h = n & 1;
-        if (!wait(sm.p_ready[h], (uint32_t)(n / 2)) || !wait(sm.v_full[s], (uint32_t)(n / AT_RING))) return;
+        const int s = n % RING, h = n & 1;
+        if (!wait(sm.p_ready[h], (uint32_t)(n / 2))) return;
         if (n >= 2 && !wait(sm.o_free[h], (uint32_t)(n / 2 - 1))) return;
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < AT_T / 32; ++k) {
-          const uint64_t da = (HD == 128 ? umma_desc_sw128_mn(v_ring + (uint32_t)(s * TILE), 1024u, 1024u) : desc_sw64(v_ring + (uint32_t)(s * TILE))) +
-                              (uint64_t)(k * 32 * HD / 16);
+          const uint64_t da = desc_rows<HD>(ring + (uint32_t)(s * TILE + GROUP + k * 8 * GROUP), 2 * GROUP);
           const uint64_t db = umma_desc_sw128(p_tile + (uint32_t)(h * N * AT_T)) + (uint64_t)(k * 2);
           umma_f8(o_tmem + (uint32_t)(h * N), da, db, idesc_o, k > 0 ? 1u : 0u);
         }
-        umma_commit(smem_u32(&sm.v_empty[s]));
+        umma_commit(smem_u32(&sm.empty[s]));
         umma_commit(smem_u32(&sm.p_free[h]));
         umma_commit(smem_u32(&sm.o_full[h]));
       };
       int n = 0, n_q = 0;
-      Item x = {}, last = {};
-      for (int it = item_lo; it < item_hi && !failed; ++it) {
-        x = locate(it);
-        if (it == item_lo || !same_query(x, last)) {
+      for (; x.it < item_hi && !failed; next_item()) {
+        if (x.new_query) {
           if (n_q > 0) umma_commit(smem_u32(&sm.q_free[(n_q - 1) & 1]));   // every score product with the query tile before has been issued
           if (!wait(sm.q_ready[n_q & 1], (uint32_t)(n_q / 2))) break;
           ++n_q;
         }
         const uint32_t q_at = q_tile + (uint32_t)((n_q - 1) & 1) * Q_TILE;
-        last = x;
         for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
-          const int s = n % AT_RING, h = n & 1;
-          if (!wait(sm.k_full[s], (uint32_t)(n / AT_RING))) break;
+          const int s = n % RING, h = n & 1;
+          if (!wait(sm.full[s], (uint32_t)(n / RING))) break;
           if (n >= 2 && !wait(sm.s_free[h], (uint32_t)(n / 2 - 1))) break;
           tc_fence_after();
 #pragma unroll
           for (int k = 0; k < HD / 32; ++k)
-            umma_f8(s_tmem + (uint32_t)(h * NQ), desc_hd<HD>(k_ring + (uint32_t)(s * TILE)) + (uint64_t)(k * 2), desc_hd<HD>(q_at) + (uint64_t)(k * 2),
+            umma_f8(s_tmem + (uint32_t)(h * NQ), desc_rows<HD>(ring + (uint32_t)(s * TILE), 2 * GROUP) + (uint64_t)(k * 2),
+                    desc_rows<HD>(q_at, GROUP) + (uint64_t)(k * 2),
                     idesc_s, k > 0 ? 1u : 0u);
-          umma_commit(smem_u32(&sm.k_empty[s]));
           umma_commit(smem_u32(&sm.s_full[h]));
           if (n > 0) output(n - 1);
         }
@@ -414,16 +422,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     // row piece * C + column, hd bytes, swizzled as the keys are; a warp per column, hd / 32 values a lane
     constexpr int EPL = HD / 32;
     int n_q = 0;
-    Item x = {}, last = {};
-    for (int it = item_lo; it < item_hi && !failed; ++it) {
-      x = locate(it);
-      if (it > item_lo && same_query(x, last)) continue;
-      last = x;
+    for (; x.it < item_hi && !failed; next_item()) {
+      if (!x.new_query) continue;
       if (n_q > 1 && !wait_all(sm.q_free[n_q & 1], (uint32_t)(n_q / 2 - 1))) break;
       uint8_t *q_at = q_ptr + (n_q & 1) * Q_TILE;
-      const int cols = x.ni * G;
+      const int cols = x.n * G;
       for (int c = warp - 2; c < cols; c += 2) {
-        const T *src = (const T *)a.q + (long long)(rp.first + x.i0 + c / G) * a.q_t + (long long)(x.g * G + c % G) * a.q_h + lane * EPL;
+        const T *src = (const T *)a.q + (long long)(x.first + c / G) * a.q_t + (long long)(x.g * G + c % G) * a.q_h + lane * EPL;
         float v[EPL];
         if (EPL == 4) {
           const uint2 u = __ldg(reinterpret_cast<const uint2 *>(src));
@@ -473,28 +478,25 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     }
   } else if (warp < 12) {
     // ---------------- softmax: group 0 takes the even tiles, group 1 the odd ones ----------------
-    const int grp = warp >= 8 ? 1 : 0, wq = warp & 3, tok = wq * 32 + lane, pg = tok / a.block;
+    const int grp = warp >= 8 ? 1 : 0, wq = warp & 3, tok = wq * 32 + lane, pg = tok >> shift;
     const uint32_t s_lane = s_tmem + ((uint32_t)(32 * wq) << 16) + (uint32_t)(grp * NQ);
     float4 *ab = sm.ab[warp - 4];
     float l[C];
     float m_run = AT_LOW;                             // lane c: the running frame of column c
     int n = 0, n_q = -1, k = 0;                       // k: tiles this group has done
-    Item x = {}, last = {};
-    for (int it = item_lo; it < item_hi && !failed; ++it) {
-      x = locate(it);
-      if (it == item_lo || !same_query(x, last)) ++n_q;
-      last = x;
-      const int cols = x.ni * G;
+    for (; x.it < item_hi && !failed; next_item()) {
+      if (x.new_query) ++n_q;
+      const int cols = x.n * G;
 #pragma unroll
       for (int c = 0; c < C; ++c) l[c] = 0.f;
       m_run = AT_LOW;
-      const int lim0 = rp.c - rp.n + x.i0, lim1 = lim0 + x.ni - 1;
+      const int lim0 = x.c - x.n, lim1 = x.c - 1;          // last index that the first and the last new token see
       for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
         if ((n & 1) != grp) continue;
         const int j = t * AT_T + tok;
-        if (!wait_all(sm.e_full[n % AT_EXPS], (uint32_t)(n / AT_EXPS))) break;
-        const float ek = pow2f(sm.exps[n % AT_EXPS][0][pg]);
-        const int ev_i = sm.exps[n % AT_EXPS][1][pg];
+        if (!wait_all(sm.e_full[n % EXPS], (uint32_t)(n / EXPS))) break;
+        const float ek = pow2f(sm.exps[n % EXPS][0][pg]);
+        const int ev_i = sm.exps[n % EXPS][1][pg];
         const float ev = (float)ev_i;
         if (!wait_all(sm.s_full[grp], (uint32_t)k)) break;
         tc_fence_after();
@@ -590,11 +592,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
           }
         }
         // the values of a token that no column sees may be anything (its page may not even have been read): zeros
-        if ((t + 1) * AT_T > rp.c || masked) {
-          const int s = n % AT_RING;
-          if (!wait_all(sm.v_full[s], (uint32_t)(n / AT_RING))) break;
+        if (masked) {
+          const int s = n % RING;
+          if (!wait_all(sm.full[s], (uint32_t)(n / RING))) break;
           if (unseen) {
-            uint4 *z = reinterpret_cast<uint4 *>(base_ptr + (v_ring - base) + s * TILE + tok * HD);
+            uint4 *z = reinterpret_cast<uint4 *>(base_ptr + s * TILE + (tok >> 3) * 2 * GROUP + GROUP + (tok & 7) * HD);
 #pragma unroll
             for (int i = 0; i < HD / 16; ++i) z[i] = make_uint4(0u, 0u, 0u, 0u);
           }
@@ -606,7 +608,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       }
       if (failed) break;
       // the item's sums: over the lanes, then over the warps
-      const int ii = it - item_lo, h = ii & 1;
+      const int ii = x.it - item_lo, h = ii & 1;
       if (ii >= 2 && !wait_all(sm.l_free[h], (uint32_t)(ii / 2 - 1))) break;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -628,9 +630,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     float4 *ab = sm.ab[warp - 4];
     float o[C];
     int n = 0;
-    for (int it = item_lo; it < item_hi && !failed; ++it) {
-      const Item x = locate(it);
-      const int cols = x.ni * G;
+    for (; x.it < item_hi && !failed; next_item()) {
+      const int cols = x.n * G;
       float m_run = AT_LOW;                           // lane c: the running frame of column c
 #pragma unroll
       for (int c = 0; c < C; ++c) o[c] = 0.f;
@@ -668,7 +669,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         if (lane == 0) mbar_arrive(smem_u32(&sm.o_free[h]));
       }
       if (failed) break;
-      const int ii = it - item_lo, h = ii & 1;
+      const int ii = x.it - item_lo, h = ii & 1;
       if (!wait_all(sm.l_ready[h], (uint32_t)(ii / 2))) break;
       float L = 0.f;                                  // lane c: the sum of column c in the frame m_run
       if (lane < C) {
@@ -683,13 +684,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.l_free[h]));
       const long long bg = (long long)x.b * a.n_kv + x.g;
-      if (rp.ns == 1) {
+      if (x.ns == 1) {
         const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           const float f = __shfl_sync(0xffffffffu, inv, c);
           if (c < cols && has_dim)
-            ((T *)a.out)[(long long)(rp.first + x.i0 + c / G) * a.o_t + (long long)(x.g * G + c % G) * a.o_h + d] = from_f32<T>(o[c] * f);
+            ((T *)a.out)[(long long)(x.first + c / G) * a.o_t + (long long)(x.g * G + c % G) * a.o_h + d] = from_f32<T>(o[c] * f);
         }
         if (a.mass && wq == 0 && lane < cols) a.ml[bg * a.cols + lane] = make_float2(m_run - 8.f, inv);
       } else {
@@ -719,9 +720,9 @@ __global__ void __launch_bounds__(HD) attend_combine_kernel(const __grid_constan
   __shared__ float2 sml[AT_SPLITS];
   const int b = blockIdx.x / a.n_kv, g = blockIdx.x - b * a.n_kv, col = blockIdx.y, d = threadIdx.x, G = a.n_q / a.n_kv;
   const int first = a.cu ? a.cu[b] : b, end = a.cu ? a.cu[b + 1] : b + 1;
-  const RowPlan r = row_plan(a.ctx[b], first, end, a, G, 1);       // (ns does not depend on the columns of a tile)
+  const RowPlan r = row_plan(a.ctx[b], first, end, a, G);
   griddep_wait();
-  if (r.n == 0 || r.ns <= 1 || col >= r.n * G) return;
+  if (r.ns <= 1 || col >= r.n * G) return;
   const long long at = (long long)blockIdx.x * a.max_splits;
   for (int s = d; s < r.ns; s += HD) sml[s] = __ldcg(a.part_ml + (at + s) * a.cols + col);
   __syncthreads();
@@ -751,9 +752,9 @@ __global__ void __launch_bounds__(256) attend_mass_kernel(const __grid_constant_
   __shared__ float2 ml[AT_MAXC];
   const int b = blockIdx.x / a.n_kv, G = a.n_q / a.n_kv;
   const int first = a.cu ? a.cu[b] : b, end = a.cu ? a.cu[b + 1] : b + 1;
-  const RowPlan r = row_plan(a.ctx[b], first, end, a, G, 1);
+  const RowPlan r = row_plan(a.ctx[b], first, end, a, G);
   griddep_wait();
-  if (r.n == 0) return;
+  if (r.ns == 0) return;
   const int cols = r.n * G;
   if ((int)threadIdx.x < cols) ml[threadIdx.x] = __ldcg(a.ml + (long long)blockIdx.x * a.cols + threadIdx.x);
   __syncthreads();
@@ -856,7 +857,7 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
   if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   CUtensorMap tm;
-  const int rc = tma_encode_u8_rows(&tm, cache->pool, (unsigned long long)cache->pages * 2 * cache->n_kv * cache->block, cache->head_dim, cache->block);
+  const int rc = tma_encode_kv8(&tm, cache->pool, (unsigned long long)cache->pages, cache->n_kv, cache->block, cache->head_dim);
   if (rc != CORUN_OK) return rc;
   char *w = (char *)ws;
   const AttendArgs a{cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new, window < (1 << 30) ? window : 0, s.cols, s.max_splits,
