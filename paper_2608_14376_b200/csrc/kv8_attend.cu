@@ -15,13 +15,13 @@
 // share in the result; the sum of weights takes w 2^-e_v back.
 // A tile's output stays in its own frame M; it is added to the running output, held in registers, in 32 bits.
 //
-// An item is (row, tile of query columns, key head, split).  Rows with n G <= 32 columns are split into at most AT_SPLITS parts of at
-// least two tiles; rows with more are not.  The split depends on the row's own ctx, n and window alone, sums
+// An item is (row, tile of query columns, key head, split).  Rows with n G <= 32 columns are split into parts (at_splits); rows with
+// more are another kernel's.  The split depends on the row's own ctx, n and window alone, sums
 // have one fixed order, and which CTA computes an item has no influence on any value: a row's result does not depend on
 // the other rows.  Every CTA (one per SM) takes a stretch of the item list, cut by cost.
-//   warp 0        producer: block-table lookups, TMA loads, exponents
-//   warp 1        issues the MMAs: the scores of tile n + 1 before the output product of tile n
-//   warps 2, 3    query tile of the next item
+//   warps 0, 3    producers of the even / odd tiles: block-table lookups, TMA loads, exponents
+//   warp 1        issues the MMAs: the scores of tile n + 2 before the output product of tile n
+//   warp 2        query tiles, up to two ahead
 //   warps 4-7, 8-11   softmax of even / odd tiles, a thread per cached token
 //   warps 12-15   output: a thread per value dim
 // A second kernel combines a row's splits in ascending order, a third one adds up the weights from the scores that the
@@ -38,7 +38,7 @@ namespace {
 
 constexpr int AT_MAXB = 1024;       // rows per call
 constexpr int AT_T = 128;           // tokens per tile
-constexpr int AT_SPLITS = 64;       // splits of a row at most
+constexpr int AT_SPLITS = 128;      // splits of a row at most
 constexpr int AT_MIN_TILES = 2;     // tiles of a split at least
 constexpr int AT_MAXC = 32;         // columns of a tile at most; rows with as many columns or fewer are split
 // Tiles (keys and values) in shared memory: as many as fit beside the columns' operands.
@@ -50,7 +50,7 @@ constexpr float AT_LOW = -1e30f;    // a maximum over nothing
 struct AttendArgs {
   const int8_t *exps;
   long long pages;
-  int block, n_kv, n_q, B, T, max_blocks, max_new, window, cols, max_splits;   // cols: columns per (row, key head) in the workspace
+  int block, n_kv, n_q, B, T, max_blocks, max_new, window, cols, max_splits, sms;   // cols: columns per (row, key head) in the workspace
   const int *block_table, *ctx, *cu;
   const void *q;
   void *out;
@@ -65,24 +65,30 @@ struct AttendArgs {
   long long score_tokens;
 };
 
-// What a row asks for: its new tokens (0 = left out), the tiles it reads, its splits of tps tiles (0 = not this kernel's).
+// What a row asks for: its new tokens (0 = left out), the tiles [t_lo, t_hi) it reads, its splits (0 = not this kernel's).
 struct RowPlan {
-  int c, n, first, t_lo, t_hi, ns, tps;
+  int c, n, first, t_lo, t_hi, ns;
 };
-__device__ __forceinline__ int at_tps(int tiles) { return max(AT_MIN_TILES, (tiles + AT_SPLITS - 1) / AT_SPLITS); }
 __device__ __forceinline__ int at_lo(int c, int n, int window) { return window ? max(0, c - n - window + 1) / AT_T : 0; }
+// Splits of a row that reads `tiles` tiles: two tiles each or more, and where one row's splits alone fill the SMs, a whole number
+// of rounds of them (two rows of 100003 tokens and 4 key heads: 3 rounds of 37 * 4 splits of 7 or 8 tiles each).  The s-th split
+// begins floor(tiles * s / ns) tiles behind t_lo.
+__host__ __device__ inline int at_splits(int tiles, int n_kv, int sms) {
+  int ns = tiles / AT_MIN_TILES;
+  ns = ns < 1 ? 1 : ns > AT_SPLITS ? AT_SPLITS : ns;
+  const int rounds = (int)((long long)ns * n_kv / sms);
+  return rounds > 0 ? (rounds * sms / n_kv > 0 ? rounds * sms / n_kv : 1) : ns;
+}
 __device__ __forceinline__ RowPlan row_plan(int c, int first, int end, const AttendArgs &a, int G) {
   RowPlan r;
   r.c = c;
   r.first = first;
   r.n = end - first;
   const bool ok = c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && r.n > 0 && r.n <= a.max_new && end <= a.T;
-  if (!ok) { r.n = 0; r.ns = 0; r.t_lo = r.t_hi = 0; r.tps = 1; return r; }
+  if (!ok) { r.n = 0; r.ns = 0; r.t_lo = r.t_hi = 0; return r; }
   r.t_lo = at_lo(c, r.n, a.window);
   r.t_hi = (c + AT_T - 1) / AT_T;
-  const int nt = r.t_hi - r.t_lo;
-  r.tps = at_tps(nt);
-  r.ns = (long long)r.n * G <= AT_MAXC ? (nt + r.tps - 1) / r.tps : 0;
+  r.ns = (long long)r.n * G <= AT_MAXC ? at_splits(r.t_hi - r.t_lo, a.n_kv, a.sms) : 0;
   return r;
 }
 
@@ -106,6 +112,18 @@ __device__ __forceinline__ float warp_max(float x) {
   float y;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
+}
+// Whether a barrier's phase is over, without waiting (try_wait may hold the thread for a while).
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -138,7 +156,7 @@ template <int C>
 struct Smem {
   static constexpr int RING = at_ring(C), EXPS = 2 * RING;         // EXPS: tiles whose exponents are held
   uint64_t full[RING], empty[RING], e_full[EXPS];
-  uint64_t q_ready[2], q_free[2], s_full[2], s_free[2], p_ready[2], p_free[2], o_full[2], o_free[2], x_bar[2], l_ready[2], l_free[2];
+  uint64_t q_ready[2], q_free[2], s_full[2], s_free[2], p_ready[2], o_full[2], o_free[2], x_bar[2], l_ready[2], l_free[2];
   uint32_t tmem;
   int abort_flag;
   int my_items[2];
@@ -148,6 +166,7 @@ struct Smem {
   float4 ab[12][C];                  // [warp - 4]: factors of old and new of every column, the tile's frame
   float lpart[2][8][C];              // [item parity][group * 4 + warp]: sums of weights
   float lframe[2][2][C];             // [item parity][group]: their frames
+  int flags[EXPS];                   // [tile] 1: a new query tile, 2: the stretch's last tile
   int8_t exps[EXPS][2][8];           // [tile][kind][page of the tile]
   int row_item[AT_MAXB + 1];         // first item of every row
   int row_ic[AT_MAXB + 1];           // cost of one of its items
@@ -188,9 +207,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     for (int s = 0; s < EXPS; ++s) mbar_init(smem_u32(&sm.e_full[s]), 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&sm.s_full[s]), 1); mbar_init(smem_u32(&sm.s_free[s]), 4);
-      mbar_init(smem_u32(&sm.p_ready[s]), 4); mbar_init(smem_u32(&sm.p_free[s]), 1);
+      mbar_init(smem_u32(&sm.p_ready[s]), 4);
       mbar_init(smem_u32(&sm.o_full[s]), 1); mbar_init(smem_u32(&sm.o_free[s]), 4);
-      mbar_init(smem_u32(&sm.q_ready[s]), 2); mbar_init(smem_u32(&sm.q_free[s]), 1);
+      mbar_init(smem_u32(&sm.q_ready[s]), 1); mbar_init(smem_u32(&sm.q_free[s]), 1);
       mbar_init(smem_u32(&sm.x_bar[s]), 4);
       mbar_init(smem_u32(&sm.l_ready[s]), 8); mbar_init(smem_u32(&sm.l_free[s]), 4);
     }
@@ -220,7 +239,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         const RowPlan p = row_plan(ctx, first, end, a, G);
         sm.row_c[r] = ctx; sm.row_first[r] = first; sm.row_n[r] = p.n;
         n = p.ns * a.n_kv;                            // 0 for a row that is left out
-        const int ic = 1 + 2 * p.tps;                 // a tile's cost is 2, an item's beyond its tiles 1
+        // a tile's cost is 2, an item's beyond its tiles 1
+        const int ic = p.ns ? 1 + (2 * (p.t_hi - p.t_lo) + p.ns - 1) / p.ns : 1;
         sm.row_ic[r] = ic;
         cst = (long long)n * ic;
       }
@@ -263,16 +283,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
   bool failed = false;
   // Where a role is in the CTA's stretch: the item (row b, key head g, split) and its tiles [t0, t1).  Going on to the next item takes
   // additions only (a division here would cost every role some hundred cycles an item).
-  struct Cursor { int it, b, g, split, ns, tps, c, n, first, t_lo, t_hi, t0, t1; bool new_query; } x = {};
+  struct Cursor { int it, b, g, split, ns, size, rest, acc, c, n, first, t_lo, t_hi, t0, t1; bool new_query; } x = {};
+  // tiles of a split: size, and one more where the remainders add up
   auto row_at = [&]() {
     x.c = sm.row_c[x.b]; x.n = sm.row_n[x.b]; x.first = sm.row_first[x.b];
+    x.ns = (sm.row_item[x.b + 1] - sm.row_item[x.b]) / a.n_kv;
     x.t_lo = at_lo(x.c, x.n, a.window);
     x.t_hi = (x.c + AT_T - 1) / AT_T;
-    x.tps = at_tps(x.t_hi - x.t_lo);
+    x.size = (x.t_hi - x.t_lo) / x.ns;
+    x.rest = (x.t_hi - x.t_lo) - x.size * x.ns;
   };
   auto tiles_at = [&]() {
-    x.t0 = x.t_lo + x.split * x.tps;
-    x.t1 = min(x.t_hi, x.t0 + x.tps);
+    x.acc += x.rest;
+    const bool one_more = x.acc >= x.ns;
+    if (one_more) x.acc -= x.ns;
+    x.t1 = x.t0 + x.size + (one_more ? 1 : 0);
   };
   x.it = item_lo;
   x.new_query = true;
@@ -284,25 +309,29 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     }
     x.b = lo;
     row_at();
-    x.ns = (sm.row_item[lo + 1] - sm.row_item[lo]) / a.n_kv;
     x.g = (item_lo - sm.row_item[lo]) / x.ns;
     x.split = item_lo - sm.row_item[lo] - x.g * x.ns;
+    x.t0 = x.t_lo + x.size * x.split + (x.rest * x.split) / x.ns;
+    x.acc = (x.rest * x.split) % x.ns;
     tiles_at();
   }
   auto next_item = [&]() {
     ++x.it;
-    x.new_query = false;
-    if (++x.split == x.ns) {
-      x.split = 0;
+    if (x.t1 < x.t_hi) {                              // the next split
+      ++x.split;
+      x.new_query = false;
+      x.t0 = x.t1;
+    } else {
+      x.split = x.acc = 0;
       x.new_query = true;
       if (++x.g == a.n_kv) {
         x.g = 0;
         if (x.it < item_hi) {
           do ++x.b; while (sm.row_item[x.b + 1] == x.it);
           row_at();
-          x.ns = (x.t_hi - x.t_lo + x.tps - 1) / x.tps;
         }
       }
+      x.t0 = x.t_lo;
     }
     tiles_at();
   };
@@ -312,24 +341,32 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     return !failed;
   };
 
-  if (warp == 0) {
-    // ---------------- producer ----------------
-    // Tiles in batches of four, eight lanes a tile and a page a lane: while a batch is loaded, the exponents of the next
-    // one and the page numbers of the one after are on their way.
+  if (warp == 0 || warp == 3) {
+    // ---------------- producers ----------------
+    // Each warp walks over all tiles and takes every other one, in batches of four, eight lanes a tile and a page a lane: while a
+    // batch is loaded, the exponents of the next one and the page numbers of the one after are on their way.
     const uint64_t pol = l2_policy_evict_normal();
-    const int per = AT_T >> shift;                   // pages of a tile
-    struct Batch { int cnt, np, g, page, ek, ev; };   // tiles; of the lane's tile: pages, key head; of its page: number, exponents
+    const int per = AT_T >> shift;                    // pages of a tile
+    struct Batch { int cnt, np, g, flags, page, ek, ev; };   // tiles; of the lane's tile: pages, key head, flags; of its page: number, exponents
     int t = x.t0, n = 0;
+    auto step = [&]() {
+      ++n;
+      if (++t >= x.t1) { next_item(); t = x.t0; }
+    };
+    if (warp == 3 && x.it < item_hi) step();
     auto pages = [&](Batch &q) {
-      q.cnt = q.np = q.g = q.ek = q.ev = 0;
+      q.cnt = q.np = q.g = q.flags = q.ek = q.ev = 0;
       const int *src = nullptr;
       for (; q.cnt < 4 && x.it < item_hi; ++q.cnt) {
+        const bool fresh = x.new_query && t == x.t0, last = x.it + 1 == item_hi && t + 1 == x.t1;
         if ((lane >> 3) == q.cnt) {
           q.np = min(per, (x.c - t * AT_T + a.block - 1) >> shift);
           q.g = x.g;
+          q.flags = (fresh ? 1 : 0) | (last ? 2 : 0);
           if ((lane & 7) < q.np) src = a.block_table + (size_t)x.b * a.max_blocks + (size_t)t * per + (lane & 7);
         }
-        if (++t >= x.t1) { next_item(); t = x.t0; }
+        step();
+        if (x.it < item_hi) step();
       }
       q.page = -1;
       if (src) q.page = load_now(src);
@@ -345,24 +382,26 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     pages(b0);
     pages(b1);
     exponents(b0);
+    int m = warp == 3 ? 1 : 0;                        // the tile that is loaded next
     while (b0.cnt > 0 && !failed) {
       exponents(b1);
       pages(b2);
       const bool page_ok = b0.page >= 0 && (long long)b0.page < a.pages;
       const int page = page_ok ? b0.page : (int)a.pages;               // behind the pool: a page outside of it reads as zeros
       const int group = b0.g * (a.block >> 3);
-      for (int i = 0; i < b0.cnt; ++i, ++n) {
-        const int s = n % RING;
-        const int np = __shfl_sync(0xffffffffu, b0.np, 8 * i);
-        if (n >= RING && !wait_all(sm.empty[s], (uint32_t)(n / RING - 1))) break;
-        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&sm.full[s]), (uint32_t)(np * a.block * 2 * HD));
-        __syncwarp();
-        if ((lane >> 3) == i && (lane & 7) < np)
-          tma_load_5d(ring + (uint32_t)(s * TILE + (lane & 7) * a.block * 2 * HD), &tm, 0, 0, 0, group, page, smem_u32(&sm.full[s]), pol);
+      for (int i = 0; i < b0.cnt; ++i, m += 2) {
+        const int s = m % RING, e = m % EXPS;
+        const bool mine = (lane >> 3) == i;
+        if (m >= RING && !wait_all(sm.empty[s], (uint32_t)(m / RING - 1))) break;
         // (the tile RING before this one has been through its output product, so the exponents twice as far back have been read)
-        const int e = n % EXPS;
-        if ((lane >> 3) == i) { sm.exps[e][0][lane & 7] = (int8_t)b0.ek; sm.exps[e][1][lane & 7] = (int8_t)b0.ev; }
+        if (mine) { sm.exps[e][0][lane & 7] = (int8_t)b0.ek; sm.exps[e][1][lane & 7] = (int8_t)b0.ev; }
+        if (mine && (lane & 7) == 0) {
+          sm.flags[e] = b0.flags;
+          mbar_arrive_expect_tx(smem_u32(&sm.full[s]), (uint32_t)(b0.np * a.block * 2 * HD));
+        }
         __syncwarp();
+        if (mine && (lane & 7) < b0.np)
+          tma_load_5d(ring + (uint32_t)(s * TILE + (lane & 7) * a.block * 2 * HD), &tm, 0, 0, 0, group, page, smem_u32(&sm.full[s]), pol);
         if (lane == 0) mbar_arrive(smem_u32(&sm.e_full[e]));
       }
       b0 = b1;
@@ -374,50 +413,59 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       // D fp32, A and B e4m3 (format 0); scores: M = 128; output: M = hd, A MN-major
       const uint32_t idesc_s = (1u << 4) | ((uint32_t)(NQ >> 3) << 17) | ((uint32_t)(AT_T >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 15) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(HD >> 4) << 24);
-      auto wait = [&](uint64_t &bar, uint32_t parity) {
-        if (!mbar_wait(smem_u32(&bar), parity & 1u, &sm.abort_flag)) failed = true;
-        return !failed;
-      };
-      auto output = [&](int n) {                      // the product of tile n's weights and values
-        const int s = n % RING, h = n & 1;
-        if (!wait(sm.p_ready[h], (uint32_t)(n / 2))) return;
-        if (n >= 2 && !wait(sm.o_free[h], (uint32_t)(n / 2 - 1))) return;
-        tc_fence_after();
-#pragma unroll
-        for (int k = 0; k < AT_T / 32; ++k) {
-          const uint64_t da = desc_rows<HD>(ring + (uint32_t)(s * TILE + GROUP + k * 8 * GROUP), 2 * GROUP);
-          const uint64_t db = umma_desc_sw128(p_tile + (uint32_t)(h * N * AT_T)) + (uint64_t)(k * 2);
-          umma_f8(o_tmem + (uint32_t)(h * N), da, db, idesc_o, k > 0 ? 1u : 0u);
-        }
-        umma_commit(smem_u32(&sm.empty[s]));
-        umma_commit(smem_u32(&sm.p_free[h]));
-        umma_commit(smem_u32(&sm.o_full[h]));
-      };
-      int n = 0, n_q = 0;
-      for (; x.it < item_hi && !failed; next_item()) {
-        if (x.new_query) {
-          if (n_q > 0) umma_commit(smem_u32(&sm.q_free[(n_q - 1) & 1]));   // every score product with the query tile before has been issued
-          if (!wait(sm.q_ready[n_q & 1], (uint32_t)(n_q / 2))) break;
-          ++n_q;
-        }
-        const uint32_t q_at = q_tile + (uint32_t)((n_q - 1) & 1) * Q_TILE;
-        for (int t = x.t0; t < x.t1 && !failed; ++t, ++n) {
-          const int s = n % RING, h = n & 1;
-          if (!wait(sm.full[s], (uint32_t)(n / RING))) break;
-          if (n >= 2 && !wait(sm.s_free[h], (uint32_t)(n / 2 - 1))) break;
+      auto is_done = [&](uint64_t &bar, int phase) { return mbar_test(smem_u32(&bar), (uint32_t)phase & 1u); };
+      // Whichever product can go on goes on: an output product as soon as its weights are there (it frees a slot of the ring), else
+      // the scores of the next tile.  The order has no influence on any value.
+      int nq = 0, no = 0, n_query = 0;                // tiles whose scores / outputs have been issued, query tiles
+      bool more = item_lo < item_hi;
+      uint32_t idle = 0;
+      uint64_t idle_from = 0;
+      while (more || no < nq) {
+        bool did = false;
+        if (no < nq && is_done(sm.p_ready[no & 1], no / 2) && (no < 2 || is_done(sm.o_free[no & 1], no / 2 - 1))) {
+          const int s = no % RING, h = no & 1;
           tc_fence_after();
 #pragma unroll
-          for (int k = 0; k < HD / 32; ++k)
-            umma_f8(s_tmem + (uint32_t)(h * NQ), desc_rows<HD>(ring + (uint32_t)(s * TILE), 2 * GROUP) + (uint64_t)(k * 2),
-                    desc_rows<HD>(q_at, GROUP) + (uint64_t)(k * 2),
-                    idesc_s, k > 0 ? 1u : 0u);
-          umma_commit(smem_u32(&sm.s_full[h]));
-          if (n > 0) output(n - 1);
+          for (int k = 0; k < AT_T / 32; ++k) {
+            const uint64_t da = desc_rows<HD>(ring + (uint32_t)(s * TILE + GROUP + k * 8 * GROUP), 2 * GROUP);
+            const uint64_t db = umma_desc_sw128(p_tile + (uint32_t)(h * N * AT_T)) + (uint64_t)(k * 2);
+            umma_f8(o_tmem + (uint32_t)(h * N), da, db, idesc_o, k > 0 ? 1u : 0u);
+          }
+          umma_commit(smem_u32(&sm.o_full[h]));
+          umma_commit(smem_u32(&sm.empty[s]));
+          ++no;
+          did = true;
+        }
+        if (more && (nq < 2 || is_done(sm.s_free[nq & 1], nq / 2 - 1)) && is_done(sm.full[nq % RING], nq / RING)) {
+          const int s = nq % RING, h = nq & 1, flags = sm.flags[nq % EXPS];
+          if (!(flags & 1) || is_done(sm.q_ready[n_query & 1], n_query / 2)) {
+            if (flags & 1) {
+              if (n_query > 0) umma_commit(smem_u32(&sm.q_free[(n_query - 1) & 1]));   // the scores with the query tile before have been issued
+              ++n_query;
+            }
+            more = !(flags & 2);
+            const uint32_t q_at = q_tile + (uint32_t)((n_query - 1) & 1) * Q_TILE;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < HD / 32; ++k)
+              umma_f8(s_tmem + (uint32_t)(h * NQ), desc_rows<HD>(ring + (uint32_t)(s * TILE), 2 * GROUP) + (uint64_t)(k * 2),
+                      desc_rows<HD>(q_at, GROUP) + (uint64_t)(k * 2), idesc_s, k > 0 ? 1u : 0u);
+            umma_commit(smem_u32(&sm.s_full[h]));
+            ++nq;
+            did = true;
+          }
+        }
+        if (did) {
+          idle = 0;
+        } else if ((++idle & 255u) == 0u) {            // bounded, as every wait
+          const uint64_t now = globaltimer_ns();
+          if (idle == 256u) idle_from = now;
+          if (*(volatile int *)&sm.abort_flag) { failed = true; break; }
+          if (now - idle_from > 2000000000ull) { *(volatile int *)&sm.abort_flag = 1; failed = true; break; }
         }
       }
-      if (n > 0 && !failed) output(n - 1);
     }
-  } else if (warp < 4) {
+  } else if (warp == 2) {
     // ---------------- query tile ----------------
     // row piece * C + column, hd bytes, swizzled as the keys are; a warp per column, hd / 32 values a lane
     constexpr int EPL = HD / 32;
@@ -427,7 +475,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       if (n_q > 1 && !wait_all(sm.q_free[n_q & 1], (uint32_t)(n_q / 2 - 1))) break;
       uint8_t *q_at = q_ptr + (n_q & 1) * Q_TILE;
       const int cols = x.n * G;
-      for (int c = warp - 2; c < cols; c += 2) {
+      for (int c = 0; c < cols; ++c) {
         const T *src = (const T *)a.q + (long long)(x.first + c / G) * a.q_t + (long long)(x.g * G + c % G) * a.q_h + lane * EPL;
         float v[EPL];
         if (EPL == 4) {
@@ -568,8 +616,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
           ab[lane] = make_float4(ex2(m_run - m_new), ex2(m_tile - m_new), m_tile - 8.f, 0.f);
           m_run = m_new;
         }
-        // P of the tile before the last must have been read, and its frames
-        if (k > 0 && !wait_all(sm.p_free[grp], (uint32_t)(k - 1))) break;
+        // the frames of the group's tile before must have been read; its output product, and so its weights, then too
         if (k > 0 && !wait_all(sm.o_free[grp], (uint32_t)(k - 1))) break;
         if (wq == 0 && lane < C) sm.frame[grp][lane] = m_tile;
         __syncwarp();
@@ -713,37 +760,74 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
   if (warp == 0) tmem_dealloc(s_tmem, TMEM_COLS);
 }
 
-// One block per (row, key head, column), one thread per dim: the row's splits in ascending order.
+// One block per (row, key head, column): each of four warps takes a quarter of the row's splits, ascending, hd / 32 dims a lane; the quarters
+// are added in their order.
+constexpr int AT_QUARTERS = 4;
+template <int W> struct alignas(4 * W) Floats { float v[W]; };
 template <typename T, int HD>
-__global__ void __launch_bounds__(HD) attend_combine_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(32 * AT_QUARTERS) attend_combine_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int W = HD / 32, AHEAD = 8;
+  typedef Floats<W> F;
   griddep_launch_dependents();
   __shared__ float2 sml[AT_SPLITS];
-  const int b = blockIdx.x / a.n_kv, g = blockIdx.x - b * a.n_kv, col = blockIdx.y, d = threadIdx.x, G = a.n_q / a.n_kv;
+  __shared__ F so[AT_QUARTERS][32];
+  __shared__ float sl[AT_QUARTERS];
+  const int b = blockIdx.x / a.n_kv, g = blockIdx.x - b * a.n_kv, col = blockIdx.y, q = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.n_q / a.n_kv;
   const int first = a.cu ? a.cu[b] : b, end = a.cu ? a.cu[b + 1] : b + 1;
   const RowPlan r = row_plan(a.ctx[b], first, end, a, G);
   griddep_wait();
   if (r.ns <= 1 || col >= r.n * G) return;
   const long long at = (long long)blockIdx.x * a.max_splits;
-  for (int s = d; s < r.ns; s += HD) sml[s] = __ldcg(a.part_ml + (at + s) * a.cols + col);
-  __syncthreads();
-  float M = AT_LOW, L = 0.f, o = 0.f;
-  for (int s = 0; s < r.ns; ++s) M = fmaxf(M, sml[s].x);
-  const float *po = a.part_o + (at * a.cols + col) * HD + d;
+  const int per = (r.ns + AT_QUARTERS - 1) / AT_QUARTERS, lo = q * per, hi = min(r.ns, lo + per);
+  const float *po = a.part_o + (at * a.cols + col) * HD + lane * W;
   const long long step = (long long)a.cols * HD;
-  for (int s0 = 0; s0 < r.ns; s0 += 8) {
-    float x[8];
+  auto load = [&](int s) {
+    F f;
+    if (W == 4) {
+      const float4 v = __ldcg(reinterpret_cast<const float4 *>(po + s * step));
+      f.v[0] = v.x; f.v[1] = v.y; f.v[2 % W] = v.z; f.v[3 % W] = v.w;
+    } else {
+      const float2 v = __ldcg(reinterpret_cast<const float2 *>(po + s * step));
+      f.v[0] = v.x; f.v[1] = v.y;
+    }
+    return f;
+  };
+  F x[AHEAD];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = s0 + e < r.ns ? __ldcg(po + (s0 + e) * step) : 0.f;
+  for (int e = 0; e < AHEAD; ++e)
+    if (lo + e < hi) x[e] = load(lo + e);
+  for (int s = threadIdx.x; s < r.ns; s += 32 * AT_QUARTERS) sml[s] = __ldcg(a.part_ml + (at + s) * a.cols + col);
+  __syncthreads();
+  float M = AT_LOW;
+  for (int s = lane; s < r.ns; s += 32) M = fmaxf(M, sml[s].x);
+  M = warp_max(M);
+  float L = 0.f;
+  F o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (s0 + e < r.ns) {
+  for (int w = 0; w < W; ++w) o.v[w] = 0.f;
+  for (int s0 = lo; s0 < hi; s0 += AHEAD) {
+#pragma unroll
+    for (int e = 0; e < AHEAD; ++e)
+      if (s0 + e < hi) {
         const float f = ex2(sml[s0 + e].x - M);
         L = fmaf(f, sml[s0 + e].y, L);
-        o = fmaf(f, x[e], o);
+#pragma unroll
+        for (int w = 0; w < W; ++w) o.v[w] = fmaf(f, x[e].v[w], o.v[w]);
+        if (s0 + e + AHEAD < hi) x[e] = load(s0 + e + AHEAD);
       }
   }
+  so[q][lane] = o;
+  if (lane == 0) sl[q] = L;
+  __syncthreads();
+  // thread = dim
+  const int d = threadIdx.x;
+  if (d >= HD) return;
+  float sum = 0.f;
+  L = 0.f;
+#pragma unroll
+  for (int e = 0; e < AT_QUARTERS; ++e) { L += sl[e]; sum += so[e][d / W].v[d % W]; }
   const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
-  ((T *)a.out)[(long long)(first + col / G) * a.o_t + (long long)(g * G + col % G) * a.o_h + d] = from_f32<T>(o * inv);
+  ((T *)a.out)[(long long)(first + col / G) * a.o_t + (long long)(g * G + col % G) * a.o_h + d] = from_f32<T>(sum * inv);
   if (a.mass && d == 0) a.ml[(long long)blockIdx.x * a.cols + col] = make_float2(M - 8.f, inv);
 }
 
@@ -783,8 +867,8 @@ AttendSpace attend_space(int64_t B, int max_new, int n_q, int n_kv, int hd, int 
   const int64_t reach_tiles = ((int64_t)max_blocks * block + AT_T - 1) / AT_T;
   AttendSpace s;
   s.cols = (int)(all < AT_MAXC ? all : AT_MAXC);
-  s.max_splits = (int)((reach_tiles + AT_MIN_TILES - 1) / AT_MIN_TILES);
-  if (s.max_splits > AT_SPLITS) s.max_splits = AT_SPLITS;
+  s.max_splits = (int)(reach_tiles / AT_MIN_TILES);       // at_splits gives no more
+  s.max_splits = s.max_splits < 1 ? 1 : s.max_splits > AT_SPLITS ? AT_SPLITS : s.max_splits;
   s.score_tokens = reach_tiles * AT_T;
   s.part_ml = AT_STATUS * 4;
   s.part_o = s.part_ml + up(B * n_kv * s.max_splits * s.cols * 8);
@@ -807,7 +891,7 @@ cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev,
   }
   ce = launch_k(attend_kernel<T, HD, C>, dim3(sms), dim3(AT_THREADS), smem, st, false, tm, a);
   if (ce == cudaSuccess && a.max_splits > 1) {
-    ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, a.cols), dim3(HD), 0, st, true, a);
+    ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, a.cols), dim3(32 * AT_QUARTERS), 0, st, true, a);
   }
   if (ce == cudaSuccess && a.mass) {
     int gy = (4 * sms + a.B * a.n_kv - 1) / (a.B * a.n_kv);
@@ -860,7 +944,7 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
   const int rc = tma_encode_kv8(&tm, cache->pool, (unsigned long long)cache->pages, cache->n_kv, cache->block, cache->head_dim);
   if (rc != CORUN_OK) return rc;
   char *w = (char *)ws;
-  const AttendArgs a{cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new, window < (1 << 30) ? window : 0, s.cols, s.max_splits,
+  const AttendArgs a{cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new, window < (1 << 30) ? window : 0, s.cols, s.max_splits, sms,
                      rows->block_table, rows->ctx, rows->cu, q->p, out->p, q->token_stride, q->head_stride, out->token_stride, out->head_stride,
                      scale * 1.4426950408889634f, mass, (int *)w, (float2 *)(w + s.part_ml), (float *)(w + s.part_o), (float2 *)(w + s.ml),
                      (float *)(w + s.scores), s.score_tokens};
