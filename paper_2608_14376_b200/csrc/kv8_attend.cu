@@ -26,6 +26,8 @@
 //   warps 12-15   output: a thread per value dim
 // A second kernel combines a row's splits in ascending order, a third one adds up the weights from the scores that the
 // first wrote (4 bytes per token and column, where mass is wanted).  Every wait is bounded.
+#include <stddef.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -36,14 +38,14 @@
 namespace corun {
 namespace {
 
-constexpr int AT_MAXB = 1024;       // rows per call
+constexpr int AT_THREADS = 512;
+constexpr int AT_MAXB = AT_THREADS; // rows per call: a thread plans one
 constexpr int AT_T = 128;           // tokens per tile
 constexpr int AT_SPLITS = 128;      // splits of a row at most
 constexpr int AT_MIN_TILES = 2;     // tiles of a split at least
 constexpr int AT_MAXC = 32;         // columns of a tile at most; rows with as many columns or fewer are split
 // Tiles (keys and values) in shared memory: as many as fit beside the columns' operands.
-__host__ __device__ constexpr int at_ring(int C) { return C > 16 ? 4 : 5; }
-constexpr int AT_THREADS = 512;
+__host__ __device__ constexpr int at_ring(int C) { return C > 16 ? 4 : C > 8 ? 5 : 6; }
 constexpr int AT_STATUS = 256;      // status words at the start of the workspace
 constexpr float AT_LOW = -1e30f;    // a maximum over nothing
 
@@ -113,6 +115,23 @@ __device__ __forceinline__ float warp_max(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
+// Sums over the lanes of N values each, the columns shared out on the way: lane i ends up with the sum of column i >> (5 - log2 N).
+template <int N>
+__device__ __forceinline__ float lane_sums(float (&v)[N], int lane) {
+  int off = 16;
+#pragma unroll
+  for (int n = N; n > 1; n >>= 1, off >>= 1) {
+    const bool up = lane & off;
+#pragma unroll
+    for (int i = 0; i < n / 2; ++i) {
+      const float give = up ? v[i] : v[i + n / 2], keep = up ? v[i + n / 2] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+    }
+  }
+  float s = v[0];
+  for (; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+  return s;
+}
 // Whether a barrier's phase is over, without waiting (try_wait may hold the thread for a while).
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
   uint32_t ok;
@@ -159,9 +178,9 @@ struct Smem {
   uint64_t q_ready[2], q_free[2], s_full[2], s_free[2], p_ready[2], o_full[2], o_free[2], x_bar[2], l_ready[2], l_free[2];
   uint32_t tmem;
   int abort_flag;
-  int my_items[2];
+  struct { int lo, hi, row, g, split, t0, acc; } mine;   // this CTA's items, where the first one is
   float q_mul[4][C];                 // 2^e of a query column times scale log2(e), by query tile
-  float x_max[2][2][C][4];           // [group][use parity][column][warp]: maxima of 32 tokens
+  alignas(16) float x_max[2][2][C][4];   // (read as float4) [group][use parity][column][warp]: maxima of 32 tokens
   float frame[2][C];                 // [tile parity]: the tile's frames
   float4 ab[12][C];                  // [warp - 4]: factors of old and new of every column, the tile's frame
   float lpart[2][8][C];              // [item parity][group * 4 + warp]: sums of weights
@@ -169,9 +188,9 @@ struct Smem {
   int flags[EXPS];                   // [tile] 1: a new query tile, 2: the stretch's last tile
   int8_t exps[EXPS][2][8];           // [tile][kind][page of the tile]
   int row_item[AT_MAXB + 1];         // first item of every row
-  int row_ic[AT_MAXB + 1];           // cost of one of its items
   int row_c[AT_MAXB], row_first[AT_MAXB], row_n[AT_MAXB];
-  long long row_cost[AT_MAXB + 1];   // cost of the items before the row
+  int warp_items[AT_THREADS / 32];
+  long long warp_cost[AT_THREADS / 32];
 };
 
 // Columns of a product with `pieces` columns per query column: an M = 128 MMA takes N in steps of 16.
@@ -189,6 +208,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
   constexpr int RING = at_ring(C), EXPS = 2 * RING, GROUP = 8 * HD, TILE = 2 * AT_T * HD, Q_TILE = q_bytes<T, HD, C>();
   constexpr int COLS = 2 * NQ + 2 * N;
   constexpr uint32_t TMEM_COLS = COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
+  static_assert(offsetof(Smem<C>, x_max) % 16 == 0 && offsetof(Smem<C>, ab) % 16 == 0 && alignof(Smem<C>) >= 16, "read 16 bytes at a time");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t *base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -225,61 +245,66 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
     uint4 *z = reinterpret_cast<uint4 *>(q_ptr);
     for (int i = tid - 128; i < (int)(p_tile - q_tile + 2 * N * AT_T) / 16; i += AT_THREADS - 128) z[i] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async();
-  } else if (warp == 2) {
-    // the item list: how many items, and what they cost, before every row
-    int run = 0;
-    long long crun = 0;
-    for (int r0 = 0; r0 < a.B; r0 += 32) {
-      const int r = r0 + lane;
-      int n = 0;
-      long long cst = 0;
-      if (r < a.B) {
-        const int first = a.cu ? __ldg(a.cu + r) : r, end = a.cu ? __ldg(a.cu + r + 1) : r + 1;
-        const int ctx = __ldg(a.ctx + r);
-        const RowPlan p = row_plan(ctx, first, end, a, G);
-        sm.row_c[r] = ctx; sm.row_first[r] = first; sm.row_n[r] = p.n;
-        n = p.ns * a.n_kv;                            // 0 for a row that is left out
-        // a tile's cost is 2, an item's beyond its tiles 1
-        const int ic = p.ns ? 1 + (2 * (p.t_hi - p.t_lo) + p.ns - 1) / p.ns : 1;
-        sm.row_ic[r] = ic;
-        cst = (long long)n * ic;
-      }
-      int inc = n;
-      long long cinc = cst;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, inc, o);
-        const long long cv = __shfl_up_sync(0xffffffffu, cinc, o);
-        if (lane >= o) { inc += v; cinc += cv; }
-      }
-      if (r < a.B) { sm.row_item[r] = run + inc - n; sm.row_cost[r] = crun + cinc - cst; }
-      run += __shfl_sync(0xffffffffu, inc, 31);
-      crun += __shfl_sync(0xffffffffu, cinc, 31);
+  }
+  // (programmatic launch) everything above reads nothing that another kernel writes
+  griddep_wait();
+  // the item list: a thread plans a row; items and their cost before every row by a sum over the threads
+  {
+    int items = 0, ic = 1, ns = 0, lo = 0, tiles = 0;
+    if (tid < a.B) {
+      const int first = a.cu ? __ldcg(a.cu + tid) : tid, end = a.cu ? __ldcg(a.cu + tid + 1) : tid + 1, ctx = __ldcg(a.ctx + tid);
+      const RowPlan p = row_plan(ctx, first, end, a, G);
+      sm.row_c[tid] = ctx; sm.row_first[tid] = first; sm.row_n[tid] = p.n;
+      ns = p.ns;
+      lo = p.t_lo;
+      tiles = p.t_hi - p.t_lo;
+      items = ns * a.n_kv;                            // 0 for a row that is left out
+      ic = ns ? 1 + (2 * tiles + ns - 1) / ns : 1;    // a tile's cost is 2, an item's beyond its tiles 1
     }
-    __syncwarp();
-    if (lane == 0) {
-      sm.row_item[a.B] = run;
-      sm.row_cost[a.B] = crun;
-      auto bound = [&](int k) {                       // an item goes to the CTA in whose share of the cost it starts
-        if (k >= (int)gridDim.x) return run;
-        const long long t = (crun * k + gridDim.x - 1) / gridDim.x;
-        int lo = 0, hi = a.B;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (sm.row_cost[mid] <= t) lo = mid; else hi = mid;
-        }
-        const long long i = (t - sm.row_cost[lo] + sm.row_ic[lo] - 1) / sm.row_ic[lo];
-        return (int)min((long long)sm.row_item[lo] + i, (long long)sm.row_item[lo + 1]);
-      };
-      sm.my_items[0] = bound((int)blockIdx.x);
-      sm.my_items[1] = bound((int)blockIdx.x + 1);
+    const long long cost = (long long)items * ic;
+    int inc = items;
+    long long cinc = cost;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, o);
+      const long long cv = __shfl_up_sync(0xffffffffu, cinc, o);
+      if (lane >= o) { inc += v; cinc += cv; }
+    }
+    if (lane == 31) { sm.warp_items[warp] = inc; sm.warp_cost[warp] = cinc; }
+    __syncthreads();
+    int all = 0;
+    long long call = 0;
+    inc -= items;
+    cinc -= cost;
+    for (int w = 0; w < AT_THREADS / 32; ++w) {
+      if (w < warp) { inc += sm.warp_items[w]; cinc += sm.warp_cost[w]; }
+      all += sm.warp_items[w];
+      call += sm.warp_cost[w];
+    }
+    if (tid < a.B) sm.row_item[tid] = inc;
+    if (tid == 0) sm.row_item[a.B] = all;
+    // a CTA's stretch: from the first item that starts at or behind blockIdx / gridDim of all cost, to the next CTA's
+    const long long from = (call * blockIdx.x + gridDim.x - 1) / gridDim.x, to = (call * (blockIdx.x + 1) + gridDim.x - 1) / gridDim.x;
+    if (tid == 0 && from == 0) sm.mine.lo = 0;
+    if (tid == 0 && to == 0) sm.mine.hi = 0;
+    if (cinc < from && from <= cinc + cost) sm.mine.lo = inc + (int)((from - cinc + ic - 1) / ic);
+    if (cinc < to && to <= cinc + cost) sm.mine.hi = inc + (int)((to - cinc + ic - 1) / ic);
+    __syncthreads();
+    const int i = sm.mine.lo - inc;
+    if (i >= 0 && i < items) {                        // where the first item is
+      const int split = i % ns, size = tiles / ns, rest = tiles - size * ns;
+      sm.mine.row = tid;
+      sm.mine.g = i / ns;
+      sm.mine.split = split;
+      sm.mine.t0 = lo + size * split + (rest * split) / ns;
+      sm.mine.acc = (rest * split) % ns;
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t s_tmem = sm.tmem, o_tmem = s_tmem + 2 * NQ;
-  const int item_lo = sm.my_items[0], item_hi = sm.my_items[1];
+  const int item_lo = sm.mine.lo, item_hi = sm.mine.hi;
   bool failed = false;
   // Where a role is in the CTA's stretch: the item (row b, key head g, split) and its tiles [t0, t1).  Going on to the next item takes
   // additions only (a division here would cost every role some hundred cycles an item).
@@ -302,17 +327,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
   x.it = item_lo;
   x.new_query = true;
   if (item_lo < item_hi) {
-    int lo = 0, hi = a.B;
-    while (hi - lo > 1) {                             // the row whose items hold item_lo (rows without items do not)
-      const int mid = (lo + hi) >> 1;
-      if (sm.row_item[mid] <= item_lo) lo = mid; else hi = mid;
-    }
-    x.b = lo;
+    x.b = sm.mine.row;
     row_at();
-    x.g = (item_lo - sm.row_item[lo]) / x.ns;
-    x.split = item_lo - sm.row_item[lo] - x.g * x.ns;
-    x.t0 = x.t_lo + x.size * x.split + (x.rest * x.split) / x.ns;
-    x.acc = (x.rest * x.split) % x.ns;
+    x.g = sm.mine.g;
+    x.split = sm.mine.split;
+    x.t0 = sm.mine.t0;
+    x.acc = sm.mine.acc;
     tiles_at();
   }
   auto next_item = [&]() {
@@ -657,13 +677,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       // the item's sums: over the lanes, then over the warps
       const int ii = x.it - item_lo, h = ii & 1;
       if (ii >= 2 && !wait_all(sm.l_free[h], (uint32_t)(ii / 2 - 1))) break;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float v = l[c];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0) sm.lpart[h][grp * 4 + wq][c] = v;
-      }
+      const float sum = lane_sums<C>(l, lane);
+      if ((lane & (32 / C - 1)) == 0) sm.lpart[h][grp * 4 + wq][lane / (32 / C)] = sum;
       if (wq == 0 && lane < C) sm.lframe[h][grp][lane] = m_run;
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.l_ready[h]));
@@ -889,7 +904,7 @@ cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev,
     if (ce != cudaSuccess) return ce;
     if (dev < 64) done.fetch_or(1ull << dev);
   }
-  ce = launch_k(attend_kernel<T, HD, C>, dim3(sms), dim3(AT_THREADS), smem, st, false, tm, a);
+  ce = launch_k(attend_kernel<T, HD, C>, dim3(sms), dim3(AT_THREADS), smem, st, true, tm, a);
   if (ce == cudaSuccess && a.max_splits > 1) {
     ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, a.cols), dim3(32 * AT_QUARTERS), 0, st, true, a);
   }

@@ -144,7 +144,7 @@ def test_attend_refusals(lib):
         a = dict(ok, **bad)
         assert lib.corun_kv8_attend(C.byref(cache), C.byref(rows), a["max_new"], a["q"], a["out"], a["dtype"], a["n_q"], a["scale"], a["window"],
                                     a["mass"], a["ws"], a["n"], None) == corun.EINVAL, bad
-    rows.B = rows.T = 1025
+    rows.B = rows.T = 513
     assert lib.corun_kv8_attend(C.byref(cache), C.byref(rows), 1, C.byref(x), C.byref(x), 1, 32, 0.1, 0, None, BASE, 1 << 40, None) == corun.EINVAL
     rows.B, rows.T, rows.cu = 4, 40, BASE                       # 9 tokens of 4 heads: more than the weights are added up for
     assert lib.corun_kv8_attend(C.byref(cache), C.byref(rows), 9, C.byref(x), C.byref(x), 1, 32, 0.1, 0, BASE, BASE, 1 << 40, None) == corun.EINVAL
