@@ -9,10 +9,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcorun.so")
 SOURCES = ["engine.cu", "gemm.cu", "gemm_rows.cu", "gemm_experts.cu", "gemm_pair.cu", "ops.cu", "attention.cu", "attention_prefill.cu", "attention_prefill_mla.cu", "no_alloc.cu", "sched.cu", "moe.cu", "mla_paged.cu", "mla_layer.cu", "wait_probe.cu", "microbench.cu",
-           "rope.cu", "kv8_append.cu", "kv8_attend.cu", "kv8_evict.cu"]
+           "rope.cu", "kv8_append.cu", "kv8_attend.cu", "kv8_chunk.cu", "kv8_evict.cu"]
 HEADERS = ["gemm.cuh", "ops.cuh", "ptx.cuh", "launch.cuh", "checks.cuh", os.path.join("..", "..", "include", "corun.h"),
            os.path.join("..", "..", "include", "corun_sched.h"), os.path.join("..", "..", "include", "corun_moe.h"),
-           os.path.join("..", "..", "include", "corun_mla.h"), os.path.join("..", "..", "include", "corun_debug.h"), "moe.cuh", "mla.cuh", "kv8.cuh",
+           os.path.join("..", "..", "include", "corun_mla.h"), os.path.join("..", "..", "include", "corun_debug.h"), "moe.cuh", "mla.cuh", "kv8.cuh", "kv8_attend.cuh",
            os.path.join("..", "..", "include", "corun_rope.h"), os.path.join("..", "..", "include", "corun_kv8.h")]
 # CORUN_BUILD_DEBUG=1 in the environment compiles the kernel timelines in (-DCORUN_BUILD_DEBUG; see
 # include/corun_debug.h); a marker file remembers which kind the library on disk is.

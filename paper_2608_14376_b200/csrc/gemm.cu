@@ -312,14 +312,14 @@ int tma_encode_2d(CUtensorMap *m, const void *base, int is_fp16, unsigned long l
   return r == CUDA_SUCCESS ? CORUN_OK : CORUN_ECUDA;
 }
 
-int tma_encode_kv8(CUtensorMap *m, const void *base, unsigned long long pages, int n_kv, int block, int hd) {
+int tma_encode_kv8(CUtensorMap *m, const void *base, unsigned long long pages, int n_kv, int block, int hd, int kinds) {
   auto enc = get_encode();
   if (!enc) { g_last_cuda_error = 99999; return CORUN_ECUDA; }
-  if (((uintptr_t)base & 15u) || (hd != 64 && hd != 128) || block % 8 || block > 64 || block < 8 || n_kv < 1 || pages < 1) return CORUN_EINVAL;
+  if (((uintptr_t)base & 15u) || (hd != 64 && hd != 128) || block % 8 || block > 64 || block < 8 || n_kv < 1 || pages < 1 || kinds < 1 || kinds > 2) return CORUN_EINVAL;
   const cuuint64_t kind = (cuuint64_t)n_kv * block * hd;
   cuuint64_t dims[5] = {(cuuint64_t)hd, 8, 2, (cuuint64_t)n_kv * block / 8, (cuuint64_t)pages};
   cuuint64_t strides[4] = {(cuuint64_t)hd, kind, (cuuint64_t)8 * hd, 2 * kind};
-  cuuint32_t box[5] = {(cuuint32_t)hd, 8, 2, (cuuint32_t)block / 8, 1};
+  cuuint32_t box[5] = {(cuuint32_t)hd, 8, (cuuint32_t)kinds, (cuuint32_t)block / 8, 1};
   cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,

@@ -257,9 +257,10 @@ cudaError_t gemm_rows_launch(const GemmPlan &p, const CUtensorMap *tmW_override,
 // (128 bytes, 128-byte swizzle) or 16 columns (32 bytes, 32-byte swizzle).
 int tma_encode_2d(CUtensorMap *m, const void *base, int is_fp16, unsigned long long rows, int cols, int box_rows,
                   int box_cols);
-// Tensor map over the 8-bit pages [pages][keys, values][n_kv][block][hd] (bytes): a box holds one page of one key head, eight rows of
-// keys, eight rows of values, the next eight of keys, ..., swizzled by the rows' width.  Coordinates: 0, 0, 0, head * block / 8, page.
-int tma_encode_kv8(CUtensorMap *m, const void *base, unsigned long long pages, int n_kv, int block, int hd);
+// Tensor map over the 8-bit pages [pages][keys, values][n_kv][block][hd] (bytes): a box holds one page of one key head, swizzled by the
+// rows' width; kinds 2: eight rows of keys, eight rows of values, the next eight of keys, ...; kinds 1: keys or values alone.
+// Coordinates: 0, 0, kind, head * block / 8, page.
+int tma_encode_kv8(CUtensorMap *m, const void *base, unsigned long long pages, int n_kv, int block, int hd, int kinds);
 // Tensor map over fp16 data seen as a 4-dimensional array: dims[0] elements are contiguous, strides[i] is the byte
 // distance between consecutive indices of dimension i + 1 (a multiple of 16; they need not ascend); the box's
 // innermost extent is 64 elements (128 bytes, 128-byte swizzle).  The box lands in shared memory densely,

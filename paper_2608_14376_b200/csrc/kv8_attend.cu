@@ -16,7 +16,7 @@
 // A tile's output stays in its own frame M; it is added to the running output, held in registers, in 32 bits.
 //
 // An item is (row, tile of query columns, key head, split).  Rows with n G <= 32 columns are split into parts (at_splits); rows with
-// more are another kernel's.  The split depends on the row's own ctx, n and window alone, sums
+// more columns are kv8_chunk.cu's.  The split depends on the row's own ctx, n and window alone, sums
 // have one fixed order, and which CTA computes an item has no influence on any value: a row's result does not depend on
 // the other rows.  Every CTA (one per SM) takes a stretch of the item list, cut by cost.
 //   warps 0, 3    producers of the even / odd tiles: block-table lookups, TMA loads, exponents
@@ -33,39 +33,17 @@
 
 #include <math_constants.h>
 
-#include "kv8.cuh"
+#include "kv8_attend.cuh"
 
 namespace corun {
 namespace {
 
 constexpr int AT_THREADS = 512;
-constexpr int AT_MAXB = AT_THREADS; // rows per call: a thread plans one
-constexpr int AT_T = 128;           // tokens per tile
+static_assert(AT_MAXB <= AT_THREADS, "a thread plans a row");
 constexpr int AT_SPLITS = 128;      // splits of a row at most
 constexpr int AT_MIN_TILES = 2;     // tiles of a split at least
-constexpr int AT_MAXC = 32;         // columns of a tile at most; rows with as many columns or fewer are split
 // Tiles (keys and values) in shared memory: as many as fit beside the columns' operands.
 __host__ __device__ constexpr int at_ring(int C) { return C > 16 ? 4 : C > 8 ? 5 : 6; }
-constexpr int AT_STATUS = 256;      // status words at the start of the workspace
-constexpr float AT_LOW = -1e30f;    // a maximum over nothing
-
-struct AttendArgs {
-  const int8_t *exps;
-  long long pages;
-  int block, n_kv, n_q, B, T, max_blocks, max_new, window, cols, max_splits, sms;   // cols: columns per (row, key head) in the workspace
-  const int *block_table, *ctx, *cu;
-  const void *q;
-  void *out;
-  long long q_t, q_h, o_t, o_h;
-  float scale_log2e;
-  float *mass;
-  int *status;
-  float2 *part_ml;    // [B][n_kv][max_splits][cols]: frame, sum
-  float *part_o;      // [B][n_kv][max_splits][cols][hd]
-  float2 *ml;         // [B][n_kv][cols]: frame, 1 / sum (with mass)
-  float *scores;      // [B][n_kv][tokens padded to tiles][cols] (with mass)
-  long long score_tokens;
-};
 
 // What a row asks for: its new tokens (0 = left out), the tiles [t_lo, t_hi) it reads, its splits (0 = not this kernel's).
 struct RowPlan {
@@ -86,35 +64,13 @@ __device__ __forceinline__ RowPlan row_plan(int c, int first, int end, const Att
   r.c = c;
   r.first = first;
   r.n = end - first;
-  const bool ok = c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && r.n > 0 && r.n <= a.max_new && end <= a.T;
-  if (!ok) { r.n = 0; r.ns = 0; r.t_lo = r.t_hi = 0; return r; }
+  if (!at_row_ok(c, first, end, a)) { r.n = 0; r.ns = 0; r.t_lo = r.t_hi = 0; return r; }
   r.t_lo = at_lo(c, r.n, a.window);
   r.t_hi = (c + AT_T - 1) / AT_T;
   r.ns = (long long)r.n * G <= AT_MAXC ? at_splits(r.t_hi - r.t_lo, a.n_kv, a.sms) : 0;
   return r;
 }
 
-// Loads that are issued where they stand (the compiler may move an ordinary one down to its first use).
-__device__ __forceinline__ int load_now(const int *p) {
-  int v;
-  asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(v) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ int load_now(const int8_t *p) {
-  int v;
-  asm volatile("ld.global.nc.s8 %0, [%1];" : "=r"(v) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float warp_max(float x) {
-  float y;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
-}
 // Sums over the lanes of N values each, the columns shared out on the way: lane i ends up with the sum of column i >> (5 - log2 N).
 template <int N>
 __device__ __forceinline__ float lane_sums(float (&v)[N], int lane) {
@@ -281,6 +237,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       all += sm.warp_items[w];
       call += sm.warp_cost[w];
     }
+    if (all == 0) griddep_launch_dependents();        // nothing to do here: the kernel for the other rows may begin
     if (tid < a.B) sm.row_item[tid] = inc;
     if (tid == 0) sm.row_item[a.B] = all;
     // a CTA's stretch: from the first item that starts at or behind blockIdx / gridDim of all cost, to the next CTA's
@@ -398,32 +355,40 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         q.ev = load_now(a.exps + at + a.n_kv);
       }
     };
+    auto load = [&](const Batch &q, int i, int tile) {   // the keys and values of the batch's i-th tile
+      const int s = tile % RING;
+      if (tile >= RING && !wait_all(sm.empty[s], (uint32_t)(tile / RING - 1))) return;
+      const bool mine = (lane >> 3) == i;
+      if (mine && (lane & 7) == 0) {
+        sm.flags[tile % EXPS] = q.flags;
+        mbar_arrive_expect_tx(smem_u32(&sm.full[s]), (uint32_t)(q.np * a.block * 2 * HD));
+      }
+      __syncwarp();
+      const bool page_ok = q.page >= 0 && (long long)q.page < a.pages;
+      const int page = page_ok ? q.page : (int)a.pages;                // behind the pool: a page outside of it reads as zeros
+      if (mine && (lane & 7) < q.np)
+        tma_load_5d(ring + (uint32_t)(s * TILE + (lane & 7) * a.block * 2 * HD), &tm, 0, 0, 0, q.g * (a.block >> 3), page,
+                    smem_u32(&sm.full[s]), pol);
+    };
     Batch b0, b1, b2;
     pages(b0);
-    pages(b1);
+    int m = warp == 3 ? 1 : 0, ahead = 0;             // the tile that is next; tiles of b0 that are on their way already
     exponents(b0);
-    int m = warp == 3 ? 1 : 0;                        // the tile that is loaded next
+    for (; ahead < b0.cnt && m + 2 * ahead < RING; ++ahead) load(b0, ahead, m + 2 * ahead);   // into free slots: before anything else is looked up
+    pages(b1);
     while (b0.cnt > 0 && !failed) {
       exponents(b1);
       pages(b2);
-      const bool page_ok = b0.page >= 0 && (long long)b0.page < a.pages;
-      const int page = page_ok ? b0.page : (int)a.pages;               // behind the pool: a page outside of it reads as zeros
-      const int group = b0.g * (a.block >> 3);
-      for (int i = 0; i < b0.cnt; ++i, m += 2) {
-        const int s = m % RING, e = m % EXPS;
-        const bool mine = (lane >> 3) == i;
-        if (m >= RING && !wait_all(sm.empty[s], (uint32_t)(m / RING - 1))) break;
+      for (int i = 0; i < b0.cnt && !failed; ++i, m += 2) {
+        if (i >= ahead) load(b0, i, m);
+        if (failed) break;
         // (the tile RING before this one has been through its output product, so the exponents twice as far back have been read)
-        if (mine) { sm.exps[e][0][lane & 7] = (int8_t)b0.ek; sm.exps[e][1][lane & 7] = (int8_t)b0.ev; }
-        if (mine && (lane & 7) == 0) {
-          sm.flags[e] = b0.flags;
-          mbar_arrive_expect_tx(smem_u32(&sm.full[s]), (uint32_t)(b0.np * a.block * 2 * HD));
-        }
+        const int e = m % EXPS;
+        if ((lane >> 3) == i) { sm.exps[e][0][lane & 7] = (int8_t)b0.ek; sm.exps[e][1][lane & 7] = (int8_t)b0.ev; }
         __syncwarp();
-        if (mine && (lane & 7) < b0.np)
-          tma_load_5d(ring + (uint32_t)(s * TILE + (lane & 7) * a.block * 2 * HD), &tm, 0, 0, 0, group, page, smem_u32(&sm.full[s]), pol);
         if (lane == 0) mbar_arrive(smem_u32(&sm.e_full[e]));
       }
+      ahead = 0;
       b0 = b1;
       b1 = b2;
     }
@@ -956,7 +921,7 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
   if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   CUtensorMap tm;
-  const int rc = tma_encode_kv8(&tm, cache->pool, (unsigned long long)cache->pages, cache->n_kv, cache->block, cache->head_dim);
+  int rc = tma_encode_kv8(&tm, cache->pool, (unsigned long long)cache->pages, cache->n_kv, cache->block, cache->head_dim, 2);
   if (rc != CORUN_OK) return rc;
   char *w = (char *)ws;
   const AttendArgs a{cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new, window < (1 << 30) ? window : 0, s.cols, s.max_splits, sms,
@@ -966,6 +931,11 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
   cudaStream_t st = (cudaStream_t)cuda_stream;
   if (dtype == CORUN_BF16) ce = cache->head_dim == 128 ? launch_attend<__nv_bfloat16, 128>(tm, a, dev, sms, st) : launch_attend<__nv_bfloat16, 64>(tm, a, dev, sms, st);
   else ce = cache->head_dim == 128 ? launch_attend<__half, 128>(tm, a, dev, sms, st) : launch_attend<__half, 64>(tm, a, dev, sms, st);
+  if (ce == cudaSuccess && (int64_t)max_new * (n_q / cache->n_kv) > AT_MAXC) {
+    rc = tma_encode_kv8(&tm, cache->pool, (unsigned long long)cache->pages, cache->n_kv, cache->block, cache->head_dim, 1);
+    if (rc != CORUN_OK) return rc;
+    ce = launch_kv8_chunk(tm, a, cache->head_dim, dtype, dev, st);
+  }
   if (ce != cudaSuccess) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   return CORUN_OK;
 }

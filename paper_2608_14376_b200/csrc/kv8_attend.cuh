@@ -1,0 +1,65 @@
+// What the two attention kernels over the 8-bit cache share: the call's arguments and a row's plan.
+// kv8_attend.cu takes the rows with at most AT_MAXC query columns (new tokens x query heads of a key head), kv8_chunk.cu the others; which
+// kernel takes a row depends on that row alone.
+#pragma once
+#include "kv8.cuh"
+
+namespace corun {
+
+constexpr int AT_T = 128;           // cached tokens per tile
+constexpr int AT_MAXC = 32;         // columns of a row that is split over its cached tokens
+constexpr int AT_MAXB = 512;        // rows per call: a thread plans one
+constexpr int AT_STATUS = 256;      // status words at the start of the workspace
+constexpr float AT_LOW = -1e30f;    // a maximum over nothing
+
+struct AttendArgs {
+  const int8_t *exps;
+  long long pages;
+  int block, n_kv, n_q, B, T, max_blocks, max_new, window, cols, max_splits, sms;   // cols: columns per (row, key head) in the workspace
+  const int *block_table, *ctx, *cu;
+  const void *q;
+  void *out;
+  long long q_t, q_h, o_t, o_h;
+  float scale_log2e;
+  float *mass;
+  int *status;
+  float2 *part_ml;    // [B][n_kv][max_splits][cols]: frame, sum
+  float *part_o;      // [B][n_kv][max_splits][cols][hd]
+  float2 *ml;         // [B][n_kv][cols]: frame, 1 / sum (with mass)
+  float *scores;      // [B][n_kv][tokens padded to tiles][cols] (with mass)
+  long long score_tokens;
+};
+
+#ifdef __CUDACC__
+// Whether a row of the call takes part.
+__device__ __forceinline__ bool at_row_ok(int c, int first, int end, const AttendArgs &a) {
+  const int n = end - first;
+  return c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && n > 0 && n <= a.max_new && end <= a.T;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Loads that are issued where they stand (the compiler may move an ordinary one down to its first use).
+__device__ __forceinline__ int load_now(const int *p) {
+  int v;
+  asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ int load_now(const int8_t *p) {
+  int v;
+  asm volatile("ld.global.nc.s8 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+#endif
+
+// Rows with more than AT_MAXC columns.  tm: tensor map whose boxes hold one page of one head and kind.  dtype: CORUN_BF16 or CORUN_F16.
+cudaError_t launch_kv8_chunk(const CUtensorMap &tm, const AttendArgs &a, int head_dim, int dtype, int dev, cudaStream_t st);
+
+}  // namespace corun
