@@ -10,7 +10,7 @@
 // With 128 rows to a tile the products are many times the cache's bytes: here the 8-bit values are turned into fp16 once per tile and
 // block (exactly; the scales stay apart), and a weight or a query is one fp16 value, where the kernel for few columns
 // takes three e4m3 ones.  The output warps do that turning: they would else wait for the MMAs most of the time.
-//   the output of block j - 1, the values of block j, the keys of block j + 2
+//   the output of block j - 1, the values of block j + 1, the keys of block j + 2
 // in turn, beside the products in their order: values of j, scores of j + 2.
 // A query row is brought to [256, 512) by a power of two before it is rounded to fp16: exact for bf16, and for fp16, but for values
 // some 2^-22 of the row's largest.
@@ -36,27 +36,25 @@ template <int HD>
 struct ChunkLayout {
   static constexpr int T8 = AT_T * HD;             // an 8-bit tile
   static constexpr int T16 = 2 * T8;               // the same in fp16: [64 dims][128 tokens x 128 bytes]
-  static constexpr int Q = 0, K16 = T16, V16 = K16 + 2 * T16, K8 = V16 + T16, V8 = K8 + CH_KR * T8;
+  static constexpr int Q = 0, K16 = T16, V16 = K16 + T16, K8 = V16 + 2 * T16, V8 = K8 + CH_KR * T8;
   static constexpr int SMEM = V8 + CH_VR * T8 + 1024;
   static constexpr uint32_t P_COL = 256, O_COL = 384;
 };
 
-// 16 e4m3 values as 16 fp16 values.
-__device__ __forceinline__ void widen(const uint4 &x, uint4 &lo, uint4 &hi) {
-  auto two = [](uint32_t v) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)v, __NV_E4M3);
-    return (uint32_t)h.x | ((uint32_t)h.y << 16);
-  };
-  lo = make_uint4(two(x.x & 0xffffu), two(x.x >> 16), two(x.y & 0xffffu), two(x.y >> 16));
-  hi = make_uint4(two(x.z & 0xffffu), two(x.z >> 16), two(x.w & 0xffffu), two(x.w >> 16));
+// Two e4m3 values as two fp16 values, exactly.
+__device__ __forceinline__ uint32_t widen2(uint16_t v) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
+  return r;
 }
+__device__ __forceinline__ uint2 widen4(uint32_t v) { return make_uint2(widen2((uint16_t)v), widen2((uint16_t)(v >> 16))); }
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ AttendArgs a) {
   using L = ChunkLayout<HD>;
   constexpr int KSTEPS = HD / 16;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t k8_full[CH_KR], k8_empty[CH_KR], v8_full[CH_VR], v8_empty[CH_VR], e_full[CH_EXPS], k_ready[2], v_ready, s_full[2],
+  __shared__ __align__(8) uint64_t k8_full[CH_KR], k8_empty[CH_KR], v8_full[CH_VR], v8_empty[CH_VR], e_full[CH_EXPS], k_ready, v_ready[2], s_full[2],
       p_ready[2], o_full, o_free, c_ready[4];
   __shared__ float max_s[4][128], sum_s[4][128];    // a block's frame and sum per row, four blocks in turn
   __shared__ float q_mul[128];                      // 2^e of a query row times scale log2(e)
@@ -74,11 +72,11 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     for (int i = 0; i < CH_VR; ++i) { mbar_init(smem_u32(&v8_full[i]), 1); mbar_init(smem_u32(&v8_empty[i]), 8); }
     for (int i = 0; i < CH_EXPS; ++i) mbar_init(smem_u32(&e_full[i]), 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&k_ready[i]), 8);          // keys in fp16
+      mbar_init(smem_u32(&v_ready[i]), 8);          // values in fp16
       mbar_init(smem_u32(&s_full[i]), 1);           // scores in TMEM
       mbar_init(smem_u32(&p_ready[i]), 128);        // every row thread has read them and written its weights
     }
-    mbar_init(smem_u32(&v_ready), 8);
+    mbar_init(smem_u32(&k_ready), 8);               // keys in fp16
     mbar_init(smem_u32(&o_full), 1);
     mbar_init(smem_u32(&o_free), 256);
     for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&c_ready[i]), 128);         // the rows' frames and sums of a block
@@ -222,25 +220,25 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       };
       auto scores = [&](int j) {
         const int b = j & 1;
-        if (!wait(k_ready[b], (uint32_t)(j >> 1))) return;
+        if (!wait(k_ready, (uint32_t)j)) return;
         tc_fence_after();
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks)
           umma_bf16(tmem + (uint32_t)b * 128, umma_desc_sw128(base + (uint32_t)(L::Q + (ks >> 2) * (128 * 128))) + (uint64_t)((ks & 3) * 2),
-                    umma_desc_sw128(base + (uint32_t)(L::K16 + b * L::T16 + (ks >> 2) * (128 * 128))) + (uint64_t)((ks & 3) * 2), idesc_s, ks > 0 ? 1u : 0u);
+                    umma_desc_sw128(base + (uint32_t)(L::K16 + (ks >> 2) * (128 * 128))) + (uint64_t)((ks & 3) * 2), idesc_s, ks > 0 ? 1u : 0u);
         umma_commit(smem_u32(&s_full[b]));
       };
       scores(0);
       if (n_blocks > 1 && !failed) scores(1);
       for (int j = 0; j < n_blocks && !failed; ++j) {
         const int b = j & 1;
-        if (!wait(p_ready[b], (uint32_t)(j >> 1)) || !wait(v_ready, (uint32_t)j)) break;
+        if (!wait(p_ready[b], (uint32_t)(j >> 1)) || !wait(v_ready[b], (uint32_t)(j >> 1))) break;
         if (j > 0 && !wait(o_free, (uint32_t)(j - 1))) break;
         tc_fence_after();
         const uint32_t p = tmem + L::P_COL + (uint32_t)b * 64;
 #pragma unroll
         for (int i = 0; i < AT_T / 16; ++i)         // 16 tokens of weights are 8 columns
-          umma_f16_ts(tmem + L::O_COL, p + (uint32_t)(8 * i), umma_desc_sw128_mn(base + (uint32_t)(L::V16 + i * 2048), 128 * 128, 1024u), idesc_o, i > 0 ? 1u : 0u);
+          umma_f16_ts(tmem + L::O_COL, p + (uint32_t)(8 * i), umma_desc_sw128_mn(base + (uint32_t)(L::V16 + b * L::T16 + i * 2048), 128 * 128, 1024u), idesc_o, i > 0 ? 1u : 0u);
         umma_commit(smem_u32(&o_full));
         if (j + 2 < n_blocks) scores(j + 2);
       }
@@ -328,21 +326,26 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     float o[HH], mx = -CUDART_INF_F, l = 0.f;
 #pragma unroll
     for (int i = 0; i < HH; ++i) o[i] = 0.f;
-    // 256 threads turn a tile: eight (four) neighbouring lanes take a token's row; the second piece of 16 bytes goes first for the
-    // upper half of the dims, so that the lanes of a row do not meet in a bank
+    // 256 threads turn a tile.  Eight neighbouring lanes take four pieces of two neighbouring tokens: the two stores of a lane then go to
+    // even positions of one row and odd ones of the next, all banks (with 128 dims the load meets twice in a bank).
+    constexpr int TOKENS = 256 / CPR;               // tokens at a time
+    const int tc = (ot & 3) + (HD == 128 ? (ot >> 5 & 1) * 4 : 0), tt = (ot >> 2 & 7) + (HD == 128 ? (ot >> 6) * 8 : (ot >> 5) * 8);
+    const int t_from = tt * HD + (HD == 128 ? ((tc ^ (tt & 7)) << 4) : ((tc ^ ((tt >> 1) & 3)) << 4));
+    const int t_to = (tc >> 2) * (128 * 128) + tt * 128, t_at0 = t_to + ((((tc & 3) * 2) ^ (tt & 7)) << 4), t_at1 = t_to + ((((tc & 3) * 2 + 1) ^ (tt & 7)) << 4);
     auto turn = [&](int from, int to, int t_lo, int t_hi) {         // tokens outside of [t_lo, t_hi) become zeros
+      uint4 x[AT_T / TOKENS];
 #pragma unroll
-      for (int k = 0; k < AT_T * CPR / 256; ++k) {
-        const int u = k * 256 + ot, t = u / CPR, c = u % CPR;
-        uint4 x = *reinterpret_cast<const uint4 *>(base_ptr + from + t * HD + (HD == 128 ? ((c ^ (t & 7)) << 4) : ((c ^ ((t >> 1) & 3)) << 4)));
-        if (t < t_lo || t >= t_hi) x = make_uint4(0u, 0u, 0u, 0u);
-        uint4 w[2];
-        widen(x, w[0], w[1]);
-        const int half = c >> 2, flip = HD == 128 ? half : (t & 1);
-        uint8_t *row = base_ptr + to + half * (128 * 128) + t * 128;
-        const uint4 first = flip ? w[1] : w[0], second = flip ? w[0] : w[1];
-        *reinterpret_cast<uint4 *>(row + ((((c & 3) * 2 + flip) ^ (t & 7)) << 4)) = first;
-        *reinterpret_cast<uint4 *>(row + ((((c & 3) * 2 + 1 - flip) ^ (t & 7)) << 4)) = second;
+      for (int k = 0; k < AT_T / TOKENS; ++k) x[k] = *reinterpret_cast<const uint4 *>(base_ptr + from + t_from + k * TOKENS * HD);
+      if (t_lo > 0 || t_hi < AT_T) {
+#pragma unroll
+        for (int k = 0; k < AT_T / TOKENS; ++k)
+          if (tt + k * TOKENS < t_lo || tt + k * TOKENS >= t_hi) x[k] = make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int k = 0; k < AT_T / TOKENS; ++k) {
+        const uint2 w0 = widen4(x[k].x), w1 = widen4(x[k].y), w2 = widen4(x[k].z), w3 = widen4(x[k].w);
+        *reinterpret_cast<uint4 *>(base_ptr + to + t_at0 + k * TOKENS * 128) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+        *reinterpret_cast<uint4 *>(base_ptr + to + t_at1 + k * TOKENS * 128) = make_uint4(w2.x, w2.y, w3.x, w3.y);
       }
       fence_proxy_async();
       __syncwarp();
@@ -350,9 +353,16 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     auto turn_keys = [&](int j) {
       const int buf = j % CH_KR;
       if (!wait_all(k8_full[buf], (uint32_t)(j / CH_KR))) return;
-      if (j > 1 && !wait_all(s_full[j & 1], (uint32_t)((j - 2) >> 1))) return;   // the scores of block j - 2 have read their keys
-      turn(L::K8 + buf * L::T8, L::K16 + (j & 1) * L::T16, 0, AT_T);
-      if (lane == 0) { mbar_arrive(smem_u32(&k8_empty[buf])); mbar_arrive(smem_u32(&k_ready[j & 1])); }
+      if (j > 0 && !wait_all(s_full[(j - 1) & 1], (uint32_t)((j - 1) >> 1))) return;   // the scores of block j - 1 have read their keys
+      turn(L::K8 + buf * L::T8, L::K16, 0, AT_T);
+      if (lane == 0) { mbar_arrive(smem_u32(&k8_empty[buf])); mbar_arrive(smem_u32(&k_ready)); }
+    };
+    auto turn_values = [&](int j) {                 // (the product of block j - 2 has read its values: its output has been)
+      const int buf = j % CH_VR;
+      if (!wait_all(v8_full[buf], (uint32_t)(j / CH_VR))) return;
+      // (a token that no row sees may hold anything, its page may not even have been read)
+      turn(L::V8 + buf * L::T8, L::V16 + (j & 1) * L::T16, vis_lo - (b0 + j) * AT_T, vis_end - (b0 + j) * AT_T);
+      if (lane == 0) { mbar_arrive(smem_u32(&v8_empty[buf])); mbar_arrive(smem_u32(&v_ready[j & 1])); }
     };
     auto output = [&](int j) {
       if (!wait_all(c_ready[j & 3], (uint32_t)(j >> 2))) return;
@@ -377,15 +387,12 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       mbar_arrive(smem_u32(&o_free));
     };
     turn_keys(0);
+    if (!failed) turn_values(0);
     if (n_blocks > 1 && !failed) turn_keys(1);
     for (int j = 0; j < n_blocks && !failed; ++j) {
-      if (j > 0) output(j - 1);                     // (its product has read the values of block j - 1)
-      const int buf = j % CH_VR;
-      if (failed || !wait_all(v8_full[buf], (uint32_t)(j / CH_VR))) break;
-      // (a token that no row sees may hold anything, its page may not even have been read)
-      turn(L::V8 + buf * L::T8, L::V16, vis_lo - (b0 + j) * AT_T, vis_end - (b0 + j) * AT_T);
-      if (lane == 0) { mbar_arrive(smem_u32(&v8_empty[buf])); mbar_arrive(smem_u32(&v_ready)); }
-      if (j + 2 < n_blocks) turn_keys(j + 2);
+      if (j > 0) output(j - 1);
+      if (j + 1 < n_blocks && !failed) turn_values(j + 1);          // beside the products: values of j, scores of j + 1
+      if (j + 2 < n_blocks && !failed) turn_keys(j + 2);
     }
     if (!failed) output(n_blocks - 1);
     // through the query tile's shared memory (all MMAs have read it), then whole rows
