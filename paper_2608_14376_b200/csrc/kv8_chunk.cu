@@ -10,8 +10,8 @@
 // With 128 rows to a tile the products are many times the cache's bytes: here the 8-bit values are turned into fp16 once per tile and
 // block (exactly; the scales stay apart), and a weight or a query is one fp16 value, where the kernel for few columns
 // takes three e4m3 ones.  The output warps do that turning: they would else wait for the MMAs most of the time.
-//   the output of block j - 1, the values of block j + 1, the keys of block j + 2
-// in turn, beside the products in their order: values of j, scores of j + 2.
+//   the output of block j - 1, the keys of block j + 2, the values of block j + 1
+// in turn, beside the products.
 // A query row is brought to [256, 512) by a power of two before it is rounded to fp16: exact for bf16, and for fp16, but for values
 // some 2^-22 of the row's largest.
 //
@@ -55,16 +55,16 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
   constexpr int KSTEPS = HD / 16;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t k8_full[CH_KR], k8_empty[CH_KR], v8_full[CH_VR], v8_empty[CH_VR], e_full[CH_EXPS], k_ready, v_ready[2], s_full[2],
-      p_ready[2], o_full, o_free, c_ready[4];
+      p_ready[2], p_free[2], o_full, o_free;
   __shared__ float max_s[4][128], sum_s[4][128];    // a block's frame and sum per row, four blocks in turn
   __shared__ float q_mul[128];                      // 2^e of a query row times scale log2(e)
   __shared__ int8_t exps[CH_EXPS][2][8];
-  __shared__ int warp_tiles[CH_THREADS / 32], s_row, s_qt, s_c, s_first, s_n;
+  __shared__ int row_c[AT_MAXB], row_tiles[AT_MAXB], s_row, s_qt, s_c, s_first, s_n;
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = a.n_q / a.n_kv, TQ = 128 / G, shift = a.block == 16 ? 4 : a.block == 32 ? 5 : 6;
-  const int g = blockIdx.x, tile = (int)gridDim.y - 1 - (int)blockIdx.y;       // heads fastest, the last tiles (the most blocks) first
+  const int g = blockIdx.x, tile = blockIdx.y;      // heads fastest
   if (tid == 0) {
     abort_flag = 0;
     s_row = -1;
@@ -74,18 +74,18 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&v_ready[i]), 8);          // values in fp16
       mbar_init(smem_u32(&s_full[i]), 1);           // scores in TMEM
-      mbar_init(smem_u32(&p_ready[i]), 128);        // every row thread has read them and written its weights
+      mbar_init(smem_u32(&p_ready[i]), 128);        // every row thread has read them and written its weights, frame and sum
+      mbar_init(smem_u32(&p_free[i]), 1);           // the output product has read the weights
     }
     mbar_init(smem_u32(&k_ready), 8);               // keys in fp16
     mbar_init(smem_u32(&o_full), 1);
     mbar_init(smem_u32(&o_free), 256);
-    for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&c_ready[i]), 128);         // the rows' frames and sums of a block
     fence_mbar_init();
     fence_proxy_async();
     prefetch_tensormap(&tm);
   }
   griddep_wait();
-  // the tile's row: tiles are numbered row by row
+  // the tile's row: the rows with the longest caches first, the last tile (the most blocks) of a row first
   {
     int c = 0, first = 0, n = 0, tiles = 0;
     if (tid < a.B) {
@@ -94,17 +94,15 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       c = __ldcg(a.ctx + tid);
       n = end - first;
       if (at_row_ok(c, first, end, a) && (long long)n * G > AT_MAXC) tiles = (n + TQ - 1) / TQ;
+      row_c[tid] = c;
+      row_tiles[tid] = tiles;
     }
-    int inc = tiles;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
-    }
-    if (lane == 31) warp_tiles[warp] = inc;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) inc += warp_tiles[w];
-    if (tile < inc && tile >= inc - tiles) { s_row = tid; s_qt = tile - (inc - tiles); s_c = c; s_first = first; s_n = n; }
+    int before = 0;
+    if (tiles > 0)
+      for (int r = 0; r < a.B; ++r)
+        if (row_c[r] > c || (row_c[r] == c && r < tid)) before += row_tiles[r];
+    if (tile >= before && tile < before + tiles) { s_row = tid; s_qt = tiles - 1 - (tile - before); s_c = c; s_first = first; s_n = n; }
   }
   __syncthreads();
   griddep_launch_dependents();
@@ -210,17 +208,17 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     // ---------------- producers
     for (int j = keys ? CH_KR : CH_VR; j < n_blocks && !failed; ++j) fetch(j);
   } else if (warp == 18) {
-    // ---------------- MMA issuer: the values of block j, then the scores of block j + 2
+    // ---------------- MMA issuer: the scores of block j + 2, then the values of block j
     if (elect_one()) {
       const uint32_t idesc_s = (1u << 4) | ((uint32_t)(AT_T >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 16) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-      auto wait = [&](uint64_t &bar, uint32_t parity) {
-        if (!mbar_wait(smem_u32(&bar), parity & 1u, &abort_flag)) failed = true;
+      auto wait = [&](uint64_t &bar, int phase) {
+        if (!mbar_wait(smem_u32(&bar), (uint32_t)phase & 1u, &abort_flag)) failed = true;
         return !failed;
       };
       auto scores = [&](int j) {
         const int b = j & 1;
-        if (!wait(k_ready, (uint32_t)j)) return;
+        if (!wait(k_ready, j)) return;
         tc_fence_after();
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks)
@@ -232,15 +230,16 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       if (n_blocks > 1 && !failed) scores(1);
       for (int j = 0; j < n_blocks && !failed; ++j) {
         const int b = j & 1;
-        if (!wait(p_ready[b], (uint32_t)(j >> 1)) || !wait(v_ready[b], (uint32_t)(j >> 1))) break;
-        if (j > 0 && !wait(o_free, (uint32_t)(j - 1))) break;
+        if (!wait(p_ready[b], j >> 1)) break;       // with its weights a block's scores have been read, too
+        if (j + 2 < n_blocks) scores(j + 2);
+        if (failed || !wait(v_ready[b], j >> 1) || (j > 0 && !wait(o_free, j - 1))) break;
         tc_fence_after();
         const uint32_t p = tmem + L::P_COL + (uint32_t)b * 64;
 #pragma unroll
         for (int i = 0; i < AT_T / 16; ++i)         // 16 tokens of weights are 8 columns
           umma_f16_ts(tmem + L::O_COL, p + (uint32_t)(8 * i), umma_desc_sw128_mn(base + (uint32_t)(L::V16 + b * L::T16 + i * 2048), 128 * 128, 1024u), idesc_o, i > 0 ? 1u : 0u);
         umma_commit(smem_u32(&o_full));
-        if (j + 2 < n_blocks) scores(j + 2);
+        umma_commit(smem_u32(&p_free[b]));
       }
     }
   } else if (warp < 8) {
@@ -279,6 +278,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
           largest(v[1], c + 1);
         }
         const float ref = bm == -CUDART_INF_F ? 0.f : bm;           // (nothing visible in this block: all its weights are 0)
+        if (j > 1 && !wait_all(p_free[sb], (uint32_t)((j >> 1) - 1))) return;
         auto weights = [&](const uint32_t (&x)[16], int c) {
           const int p = (16 * c) >> shift, ev = ex[8 + p];
           const float f = pow2f(ex[p]) * qm, off = (float)ev - ref;
@@ -311,13 +311,13 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       };
       if (__any_sync(0xffffffffu, lim < AT_T - 1 || low >= 0)) block(std::true_type{});
       else block(std::false_type{});
+      if (failed) break;
+      // (block j - 4's have been read: the product of block j - 2, which p_free has told of, waited for the output of block j - 3)
+      max_s[j & 3][tl] = bm;
+      sum_s[j & 3][tl] = l;
       tmem_st_wait();
       tc_fence_before();
       mbar_arrive(smem_u32(&p_ready[sb]));
-      // (block j - 4's have been read: its output was, before the scores of this block were issued)
-      max_s[j & 3][tl] = bm;
-      sum_s[j & 3][tl] = l;
-      mbar_arrive(smem_u32(&c_ready[j & 3]));
     }
   } else {
     // ---------------- output: one thread per row and half of the dims, in registers; and fp16 tiles of keys and values
@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       if (lane == 0) { mbar_arrive(smem_u32(&v8_empty[buf])); mbar_arrive(smem_u32(&v_ready[j & 1])); }
     };
     auto output = [&](int j) {
-      if (!wait_all(c_ready[j & 3], (uint32_t)(j >> 2))) return;
+      if (!wait_all(o_full, (uint32_t)j)) return;
+      tc_fence_after();
       // the larger frame is the scale from here on: a factor for the sums so far, or for this block
       const float bm = max_s[j & 3][tl], sum = sum_s[j & 3][tl], ref = bm == -CUDART_INF_F ? 0.f : bm;
       const bool up = bm >= mx;
@@ -373,8 +374,6 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       mx = fmaxf(mx, bm);
       l = up ? fmaf(l, factor, sum) : fmaf(sum, factor, l);
       const float f_old = up ? factor : 1.f, f_new = up ? 1.f : factor;
-      if (!wait_all(o_full, (uint32_t)j)) return;
-      tc_fence_after();
 #pragma unroll
       for (int c = 0; c < HH / 16; ++c) {
         uint32_t v[16];
@@ -391,8 +390,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     if (n_blocks > 1 && !failed) turn_keys(1);
     for (int j = 0; j < n_blocks && !failed; ++j) {
       if (j > 0) output(j - 1);
-      if (j + 1 < n_blocks && !failed) turn_values(j + 1);          // beside the products: values of j, scores of j + 1
-      if (j + 2 < n_blocks && !failed) turn_keys(j + 2);
+      if (j + 2 < n_blocks && !failed) turn_keys(j + 2);            // beside the products: scores of j + 1, values of j
+      if (j + 1 < n_blocks && !failed) turn_values(j + 1);
     }
     if (!failed) output(n_blocks - 1);
     // through the query tile's shared memory (all MMAs have read it), then whole rows
