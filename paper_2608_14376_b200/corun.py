@@ -704,46 +704,63 @@ def mla_attend(q_lat, q_rope, pool, block_table, ctx, scale: float):
 ROPE_SCALINGS = ("none", "linear", "base", "parts", "bands")
 
 
-class _Device:
-    """The tensors' device as the current one while a call is made, and torch's current stream there."""
+_torch_mod = None
 
-    def __init__(self, t):
+
+def _torch():
+    """torch, looked up once (an import statement in a call costs it half a microsecond)."""
+    global _torch_mod
+    if _torch_mod is None:
         import torch
 
-        if t.device.type != "cuda":
-            raise ValueError(f"a CUDA tensor is needed, not one on {t.device}")
-        self._torch, self._index = torch, t.device.index
-        self.stream = torch.cuda.current_stream(t.device).cuda_stream
+        _torch_mod = torch
+    return _torch_mod
 
-    def __enter__(self):
-        self._before = self._torch.cuda.current_device()
-        if self._before != self._index:
-            self._torch.cuda.set_device(self._index)
-        return self.stream
 
-    def __exit__(self, *_):
-        if self._before != self._index:
-            self._torch.cuda.set_device(self._before)
+def _stream_of(index: int) -> int:
+    """torch's current stream on device ``index``, as a ``cudaStream_t``."""
+    T = _torch()
+    raw = getattr(T._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else T.cuda.current_stream(index).cuda_stream
+
+
+def _launch(fn, where: str, device, *args):
+    """``fn(*args, stream)`` with ``device`` as the current one, on torch's current stream there."""
+    T, index = _torch(), device.index
+    if device.type != "cuda":
+        raise ValueError(f"CUDA tensors are needed, not tensors on {device}")
+    if T.cuda.current_device() != index:
+        with T.cuda.device(index):
+            rc = fn(*args, _stream_of(index))
+    else:
+        rc = fn(*args, _stream_of(index))
+    if rc:
+        raise CorunError(rc, where)
 
 
 def _dtype_code(t, what, f32=True):
-    code = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}.get(str(t.dtype), -1)
-    if code < (0 if f32 else 1):
-        raise ValueError(f"{what}: {'float32, ' if f32 else ''}bfloat16 or float16 is needed, not {t.dtype}")
-    return code
+    T, d = _torch(), t.dtype
+    if d is T.bfloat16:
+        return 1
+    if d is T.float16:
+        return 2
+    if f32 and d is T.float32:
+        return 0
+    raise ValueError(f"{what}: {'float32, ' if f32 else ''}bfloat16 or float16 is needed, not {d}")
 
 
-def _heads(t, shape, like, what):
+def _heads(t, shape, dtype, device, what):
     """[tokens, heads, dims] with contiguous dims as a ``corun_heads``."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != like.dtype or t.device != like.device or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{what}: {tuple(shape)} {like.dtype} on {like.device} with contiguous dims is needed, "
-                         f"not {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
-    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+    st = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.device != device or (st[2] != 1 and shape[2] > 1):
+        raise ValueError(f"{what}: {tuple(shape)} {dtype} on {device} with contiguous dims is needed, "
+                         f"not {tuple(t.shape)} {t.dtype} on {t.device}, strides {st}")
+    return Heads(t.data_ptr(), st[0], st[1])
 
 
 def _plain(t, shape, dtype, device, what):
     """A contiguous tensor's address."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous {tuple(shape)} {dtype} on {device} is needed, not {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
@@ -767,19 +784,16 @@ class Rope:
     def apply(self, x, positions, out=None):
         """x [tokens, heads, dims] (fp32, bf16 or fp16, any strides of tokens and heads), positions int32 [tokens] -> rotated
         values in ``out`` (default: a new tensor; may be x).  Asynchronous on torch's current stream."""
-        import torch
-
         if x.dim() != 3:
             raise ValueError(f"x: [tokens, heads, dims] is needed, not {tuple(x.shape)}")
-        code = _dtype_code(x, "x")
-        xh = _heads(x, x.shape, x, "x")
-        y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        yh = _heads(y, x.shape, x, "out")
-        pos = _plain(positions, (x.shape[0],), torch.int32, x.device, "positions")
-        with _Device(x) as st:
-            if x.numel():
-                _check(lib().corun_rope_apply(self._h, C.byref(xh), C.byref(yh), code, pos, x.shape[0], x.shape[1], x.shape[2], st),
-                       "corun_rope_apply")
+        T, code, dev = _torch(), _dtype_code(x, "x"), x.device
+        n, heads, dims = shape = x.shape
+        xh = _heads(x, shape, x.dtype, dev, "x")
+        y = out if out is not None else T.empty(shape, dtype=x.dtype, device=dev)
+        yh = _heads(y, shape, x.dtype, dev, "out")
+        pos = _plain(positions, (n,), T.int32, dev, "positions")
+        if n and heads and dims:
+            _launch(lib().corun_rope_apply, "corun_rope_apply", dev, self._h, xh, yh, code, pos, n, heads, dims)
         return y
 
     def close(self):
@@ -800,10 +814,7 @@ class Kv8Cache:
     Which pages belong to whom is the caller's to say (block tables)."""
 
     def __init__(self, pages: int, n_kv: int, head_dim: int, block: int = 16, pool=None, exps=None, device="cuda"):
-        import torch
-
-        self._torch = torch
-        shape = (pages, 2, n_kv, block, head_dim)
+        torch, shape = _torch(), (pages, 2, n_kv, block, head_dim)
         self.pool = pool if pool is not None else torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
         self.exps = exps if exps is not None else torch.zeros(shape[:3], dtype=torch.int8, device=self.pool.device)
         self.pages, self.n_kv, self.head_dim, self.block = pages, n_kv, head_dim, block
@@ -811,70 +822,64 @@ class Kv8Cache:
         self._c = Kv8CacheArgs(_plain(self.pool, shape, torch.float8_e4m3fn, self.device, "pool"),
                                _plain(self.exps, shape[:3], torch.int8, self.device, "exps"), pages, block, n_kv, head_dim)
 
-    def _rows(self, ctx, block_table, cu, T):
-        torch, dev = self._torch, self.device
-        B = ctx.shape[0]
+    def _rows(self, ctx, block_table, cu, tokens):
+        i32, dev, B = _torch().int32, self.device, ctx.shape[0]
         if block_table.dim() != 2:
             raise ValueError(f"block_table: [rows, blocks] is needed, not {tuple(block_table.shape)}")
-        return Kv8Rows(_plain(block_table, (B, block_table.shape[1]), torch.int32, dev, "block_table"), block_table.shape[1],
-                       _plain(ctx, (B,), torch.int32, dev, "ctx"), _plain(cu, (B + 1,), torch.int32, dev, "cu") if cu is not None else None, B, T)
+        blocks = block_table.shape[1]
+        return Kv8Rows(_plain(block_table, (B, blocks), i32, dev, "block_table"), blocks, _plain(ctx, (B,), i32, dev, "ctx"),
+                       _plain(cu, (B + 1,), i32, dev, "cu") if cu is not None else None, B, tokens)
 
     def _mass(self, mass, block_table):
         if mass is None:
             return None
-        return _plain(mass, (block_table.shape[0], self.n_kv, block_table.shape[1] * self.block), self._torch.float32, self.device, "mass")
+        rows, blocks = block_table.shape
+        return _plain(mass, (rows, self.n_kv, blocks * self.block), _torch().float32, self.device, "mass")
 
     def append(self, k, v, ctx, block_table, cu=None, positions=None, rope: "Rope" = None, q=None, q_out=None, mass=None):
         """Appends k, v [tokens, n_kv, head_dim]: ``ctx`` int32 [rows] counts every row's cached tokens with the new ones, ``cu``
         int32 [rows + 1] says which tokens are whose (None: one each).  ``rope`` rotates keys and q [tokens, n_q, head_dim] at
         ``positions`` int32 [tokens].  Returns the queries (``q_out``, or a new tensor), None without q; ``mass`` float32
         [rows, n_kv, blocks * block]: the new tokens' accumulated weights become 0.  Asynchronous on torch's current stream."""
-        torch = self._torch
-        T = k.shape[0]
-        code = _dtype_code(k, "k")
-        if k.device != self.device:
-            raise ValueError(f"k: a tensor on {self.device} is needed, not {k.device}")
-        kh = _heads(k, (T, self.n_kv, self.head_dim), k, "k")
-        vh = _heads(v, (T, self.n_kv, self.head_dim), k, "v")
-        rows = self._rows(ctx, block_table, cu, T)
+        T, code, dt, dev = _torch(), _dtype_code(k, "k"), k.dtype, self.device
+        n, n_kv, hd = k.shape[0], self.n_kv, self.head_dim
+        kh = _heads(k, (n, n_kv, hd), dt, dev, "k")
+        vh = _heads(v, (n, n_kv, hd), dt, dev, "v")
+        rows = self._rows(ctx, block_table, cu, n)
         qh = oh = None
         n_q = 0
         if q is not None:
             n_q = q.shape[1]
-            qh = _heads(q, (T, n_q, self.head_dim), k, "q")
+            qh = _heads(q, (n, n_q, hd), dt, dev, "q")
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            oh = _heads(q_out, (T, n_q, self.head_dim), k, "q_out")
+                q_out = T.empty((n, n_q, hd), dtype=dt, device=dev)
+            oh = _heads(q_out, (n, n_q, hd), dt, dev, "q_out")
         if rope is not None and positions is None:
             raise ValueError("rope needs positions")
-        pos = _plain(positions, (T,), torch.int32, self.device, "positions") if positions is not None else None
-        with _Device(k) as st:
-            _check(lib().corun_kv8_append(C.byref(self._c), C.byref(rows), C.byref(kh), C.byref(vh), code, rope._h if rope is not None else None,
-                                          pos, C.byref(qh) if qh is not None else None, C.byref(oh) if oh is not None else None, n_q,
-                                          self._mass(mass, block_table), st), "corun_kv8_append")
+        pos = _plain(positions, (n,), T.int32, dev, "positions") if positions is not None else None
+        _launch(lib().corun_kv8_append, "corun_kv8_append", dev, self._c, rows, kh, vh, code, rope._h if rope is not None else None, pos, qh, oh, n_q,
+                self._mass(mass, block_table))
         return q_out if q is not None else None
 
     def evict(self, ctx, block_table, mass, keep, max_keep: int, sinks: int = 4, recent: int = 64, new_ctx=None):
         """Shortens every row to its first ``sinks``, its last ``recent`` and its heaviest other tokens, ``keep`` int32 [rows] (at
         most ``max_keep``) in all, for each key head on its own.  Returns (kept int32 [rows, n_kv, max_keep]: where the tokens
         that stayed had been, then -1; new_ctx int32 [rows]).  Asynchronous on torch's current stream."""
-        torch, dev = self._torch, self.device
-        B = ctx.shape[0]
+        T, dev, B = _torch(), self.device, ctx.shape[0]
         rows = self._rows(ctx, block_table, None, B)
-        m = self._mass(mass, block_table)
-        if m is None:
+        if mass is None:
             raise ValueError("mass is needed")
-        kp = _plain(keep, (B,), torch.int32, dev, "keep")
+        m = self._mass(mass, block_table)
+        kp = _plain(keep, (B,), T.int32, dev, "keep")
         if new_ctx is None:
-            new_ctx = torch.empty_like(ctx)
-        nc = _plain(new_ctx, (B,), torch.int32, dev, "new_ctx")
-        n_ws = int(lib().corun_kv8_evict_bytes(B, self.n_kv, max_keep))
-        kept = torch.empty((B, self.n_kv, max(max_keep, 0)), dtype=torch.int32, device=dev)
+            new_ctx = T.empty_like(ctx)
+        nc = _plain(new_ctx, (B,), T.int32, dev, "new_ctx")
+        n_ws = lib().corun_kv8_evict_bytes(B, self.n_kv, max_keep)
+        kept = T.empty((B, self.n_kv, max(max_keep, 0)), dtype=T.int32, device=dev)
         # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
-        ws = torch.empty(max(n_ws, 1), dtype=torch.uint8, device=dev)
-        with _Device(self.pool) as st:
-            _check(lib().corun_kv8_evict(C.byref(self._c), rows.block_table, rows.max_blocks, B, rows.ctx, nc, m, kp, max_keep, sinks, recent,
-                                         kept.data_ptr(), ws.data_ptr(), n_ws, st), "corun_kv8_evict")
+        ws = T.empty(max(n_ws, 1), dtype=T.uint8, device=dev)
+        _launch(lib().corun_kv8_evict, "corun_kv8_evict", dev, self._c, rows.block_table, rows.max_blocks, B, rows.ctx, nc, m, kp, max_keep, sinks,
+                recent, kept.data_ptr(), ws.data_ptr(), n_ws)
         return kept, new_ctx
 
 
@@ -891,38 +896,31 @@ class Kv8Attention:
         tokens' own queries, ``cu`` int32 [rows + 1] saying which are whose (None: one each).  ``window`` > 0: a query sees that
         many tokens back, itself among them.  ``mass`` float32 [rows, n_kv, blocks * block] receives the weights.
         Asynchronous on torch's current stream."""
-        import torch
-
         rows, n_q, n_kv, hd, max_blocks, block = self.shape
-        T = q.shape[0]
-        code = _dtype_code(q, "q", f32=False)
-        if T > self.tokens or tuple(ctx.shape) != (rows,) or tuple(block_table.shape) != (rows, max_blocks) or q.device != cache.device or \
+        T, code, dt, dev, n = _torch(), _dtype_code(q, "q", f32=False), q.dtype, cache.device, q.shape[0]
+        if n > self.tokens or ctx.shape != (rows,) or block_table.shape != (rows, max_blocks) or \
                 (cache.n_kv, cache.head_dim, cache.block) != (n_kv, hd, block):
             raise ValueError(f"made for {self.tokens} tokens, {rows} rows of {max_blocks} blocks of {block} tokens, {n_kv} key heads of {hd}")
-        qh = _heads(q, (T, n_q, hd), q, "q")
+        qh = _heads(q, (n, n_q, hd), dt, dev, "q")
         if out is None:
-            out = torch.zeros((T, n_q, hd), dtype=q.dtype, device=q.device)
-        oh = _heads(out, (T, n_q, hd), q, "out")
-        r = cache._rows(ctx, block_table, cu, T)
+            out = T.zeros((n, n_q, hd), dtype=dt, device=dev)
+        oh = _heads(out, (n, n_q, hd), dt, dev, "out")
+        r = cache._rows(ctx, block_table, cu, n)
         m = cache._mass(mass, block_table)
-        L = lib()
-        key = (T, m is not None)
+        key = (n, m is not None)
         n_ws = self._bytes.get(key)
         if n_ws is None:
-            n_ws = self._bytes[key] = int(L.corun_kv8_attend_bytes(rows, T, self.max_new, n_q, n_kv, hd, block, max_blocks, int(key[1])))
+            n_ws = self._bytes[key] = lib().corun_kv8_attend_bytes(rows, n, self.max_new, n_q, n_kv, hd, block, max_blocks, int(key[1]))
         # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
-        ws = torch.empty(max(n_ws, 1), dtype=torch.uint8, device=q.device)
-        with _Device(q) as st:
-            _check(L.corun_kv8_attend(C.byref(cache._c), C.byref(r), self.max_new, C.byref(qh), C.byref(oh), code, n_q, float(scale), window, m,
-                                      ws.data_ptr(), n_ws, st), "corun_kv8_attend")
+        ws = T.empty(max(n_ws, 1), dtype=T.uint8, device=dev)
+        _launch(lib().corun_kv8_attend, "corun_kv8_attend", dev, cache._c, r, self.max_new, qh, oh, code, n_q, scale, window, m, ws.data_ptr(), n_ws)
         self.ws = ws
         return out
 
     def sync(self):
         """Waits for the stream; raises if a bounded device-side wait of the last call expired."""
         if self.ws is not None:
-            with _Device(self.ws) as st:
-                _check(lib().corun_kv8_sync(self.ws.data_ptr(), st), "corun_kv8_sync")
+            _launch(lib().corun_kv8_sync, "corun_kv8_sync", self.ws.device, self.ws.data_ptr())
 
 
 MICROBENCH_KINDS = ("rmsnorm", "softmax", "column_sum")
