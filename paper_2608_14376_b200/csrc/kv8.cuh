@@ -30,6 +30,8 @@ namespace corun {
 
 constexpr int KV8_E_MIN = -32, KV8_E_MAX = 31;
 
+// The current device and its SM count (asked of the driver once per device).
+cudaError_t device_sms(int *dev, int *sms);
 inline bool aligned_to(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 inline int dtype_size(int dtype) { return dtype == CORUN_F32 ? 4 : 2; }
 // Every head of the view starts on 16 bytes.
@@ -78,12 +80,15 @@ __device__ __forceinline__ uint32_t e4m3x4_shift(uint32_t v, float f) {
   return e4m3x2_of(a.x * f, a.y * f) | (e4m3x2_of(b.x * f, b.y * f) << 16);
 }
 
-// cos and sin of a pair at a position, times the magnitude.  The angle is formed and reduced in 64 bits: in units of half
-// turns, so that the reduction is exact.
-__device__ __forceinline__ float2 rope_cs(const RopeTable &r, int pair, int pos) {
-  double s, c;
-  sincospi((double)pos * r.half_turns[pair], &s, &c);
-  return make_float2((float)(c * (double)r.magnitude), (float)(s * (double)r.magnitude));
+// cos and sin of a pair at a position, times the magnitude.  The angle is formed and reduced in 64 bits, in half turns, so that the
+// reduction is exact; cos and sin of its first 24 bits come from 32-bit functions, and the rest r (at most 2^-25) adds its first-order
+// term (64-bit cos and sin throughout took a step's append 5 us longer).
+__device__ __forceinline__ float2 rope_cs(const RopeTable &tab, int pair, int pos) {
+  const double t = (double)pos * tab.half_turns[pair], u = t - 2.0 * rint(0.5 * t);
+  const float hi = (float)u, r = (float)(u - (double)hi) * 3.14159265f;
+  float s, c;
+  sincospif(hi, &s, &c);
+  return make_float2(fmaf(-s, r, c) * tab.magnitude, fmaf(c, r, s) * tab.magnitude);
 }
 #endif
 

@@ -43,19 +43,25 @@ __device__ __forceinline__ int row_tokens(const int *ctx, const int *cu, int b, 
 template <typename T, int EPL>
 struct alignas(sizeof(T) * EPL) LanePack { T v[EPL]; };
 
-// The lane's values of one head of one token, rotated with the token's cos and sin.
-template <typename T, int HD>
-__device__ __forceinline__ void lane_values(const T *x, const float2 *cs, int rot, bool interleaved, bool packed, float (&o)[HD / 32]) {
-  constexpr int EPL = HD / 32;
+template <typename T, int EPL>
+__device__ __forceinline__ LanePack<T, EPL> lane_load(const T *x, bool packed) {
   const int d0 = (threadIdx.x & 31) * EPL;
+  LanePack<T, EPL> p;
   if (packed) {
-    const LanePack<T, EPL> p = *reinterpret_cast<const LanePack<T, EPL> *>(x + d0);
-#pragma unroll
-    for (int e = 0; e < EPL; ++e) o[e] = to_f32(p.v[e]);
+    p = *reinterpret_cast<const LanePack<T, EPL> *>(x + d0);
   } else {
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) o[e] = to_f32(x[d0 + e]);
+    for (int e = 0; e < EPL; ++e) p.v[e] = x[d0 + e];
   }
+  return p;
+}
+
+// The lane's values of one head of one token, rotated with the token's cos and sin (x: the head in memory).
+template <typename T, int EPL>
+__device__ __forceinline__ void lane_values(const LanePack<T, EPL> &p, const T *x, const float2 *cs, int rot, bool interleaved, float (&o)[EPL]) {
+  const int d0 = (threadIdx.x & 31) * EPL;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) o[e] = to_f32(p.v[e]);
   if (rot == 0) return;
   if (interleaved) {
 #pragma unroll
@@ -95,15 +101,20 @@ __device__ __forceinline__ void store8(uint8_t *dst, const float (&x)[EPL], floa
   }
 }
 
+// AHEAD tokens of a head are requested together (16 at a time make the code so long that a CTA spends its time fetching it: a step of 64
+// rows took 17.6 us instead of 6).
 template <typename T, int HD>
 __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTable tab,
                                                             int packed) {
-  constexpr int EPL = HD / 32;
+  constexpr int EPL = HD / 32, AHEAD = 4;
+  typedef LanePack<T, EPL> P;
   extern __shared__ float2 cs[];                  // [tokens of the unit][rot / 2]
   __shared__ int s_warp[AP_WARPS], s_row, s_page, s_first, s_ctx, s_n;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long reach = (long long)a.max_blocks * a.block;
   if (tid == 0) s_row = -1;
+  griddep_wait();
+  griddep_launch_dependents();
   // which row and which of its pages: units are numbered row by row
   int before = 0;
   for (int b0 = 0; b0 < a.B; b0 += AP_THREADS) {
@@ -159,12 +170,22 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
       const long long at = (page * 2 + kind) * a.n_kv + h;
       uint8_t *dst = a.pool + at * a.block * HD + lane * EPL;
       float mx = 0.f;
-#pragma unroll 4
-      for (int t = 0; t < nt; ++t) {
-        float o[EPL];
-        lane_values<T, HD>(x + t * step, cs + t * pairs, rot, tab.interleaved, packed, o);
+      P raw[AHEAD];
+      auto request = [&](int t1) {
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) mx = fmaxf(mx, fabsf(o[e]));
+        for (int t = 0; t < AHEAD; ++t)
+          if (t1 + t < nt) raw[t] = lane_load<T, EPL>(x + (t1 + t) * step, packed);
+      };
+      for (int t1 = 0; t1 < nt; t1 += AHEAD) {
+        request(t1);
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t)
+          if (t1 + t < nt) {
+            float o[EPL];
+            lane_values<T, EPL>(raw[t], x + (t1 + t) * step, cs + (t1 + t) * pairs, rot, tab.interleaved, o);
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) mx = fmaxf(mx, fabsf(o[e]));
+          }
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -191,30 +212,42 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
       __syncwarp();
       if (lane == 0) a.exps[at] = (int8_t)e_new;
       const float f = pow2f(-e_new);
-#pragma unroll 4
-      for (int t = 0; t < nt; ++t) {
-        float o[EPL];
-        lane_values<T, HD>(x + t * step, cs + t * pairs, rot, tab.interleaved, packed, o);
-        store8<EPL>(dst + (z0 + t) * HD, o, f);
+      for (int t1 = 0; t1 < nt; t1 += AHEAD) {
+        if (nt > AHEAD) request(t1);
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t)
+          if (t1 + t < nt) {
+            float o[EPL];
+            lane_values<T, EPL>(raw[t], x + (t1 + t) * step, cs + (t1 + t) * pairs, rot, tab.interleaved, o);
+            store8<EPL>(dst + (z0 + t1 + t) * HD, o, f);
+          }
       }
     } else {
       const int h = task - 2 * a.n_kv;
       const T *x = (const T *)a.q + (long long)t0 * a.q_t + (long long)h * a.q_h;
       T *y = (T *)a.q_out + (long long)t0 * a.o_t + (long long)h * a.o_h;
-#pragma unroll 4
-      for (int t = 0; t < nt; ++t) {
-        float o[EPL];
-        lane_values<T, HD>(x + t * a.q_t, cs + t * pairs, tab.rot, tab.interleaved, packed, o);
-        __syncwarp();                             // (in place: every partner has been read)
-        if (packed) {
-          LanePack<T, EPL> p;
+      for (int t1 = 0; t1 < nt; t1 += AHEAD) {
+        P raw[AHEAD];
 #pragma unroll
-          for (int e = 0; e < EPL; ++e) p.v[e] = from_f32<T>(o[e]);
-          *reinterpret_cast<LanePack<T, EPL> *>(y + t * a.o_t + lane * EPL) = p;
-        } else {
+        for (int t = 0; t < AHEAD; ++t)
+          if (t1 + t < nt) raw[t] = lane_load<T, EPL>(x + (t1 + t) * a.q_t, packed);
 #pragma unroll
-          for (int e = 0; e < EPL; ++e) y[t * a.o_t + lane * EPL + e] = from_f32<T>(o[e]);
-        }
+        for (int t = 0; t < AHEAD; ++t)
+          if (t1 + t < nt) {
+            float o[EPL];
+            lane_values<T, EPL>(raw[t], x + (t1 + t) * a.q_t, cs + (t1 + t) * pairs, tab.rot, tab.interleaved, o);
+            __syncwarp();                           // (in place: every partner has been read)
+            T *to = y + (t1 + t) * a.o_t + lane * EPL;
+            P p;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) p.v[e] = from_f32<T>(o[e]);
+            if (packed) {
+              *reinterpret_cast<P *>(to) = p;
+            } else {
+#pragma unroll
+              for (int e = 0; e < EPL; ++e) to[e] = p.v[e];
+            }
+          }
       }
     }
   }
@@ -226,12 +259,12 @@ cudaError_t launch_append(const AppendArgs &a, const RopeTable &tab, int head_di
   long long gx = (long long)a.T / a.block + 2ll * a.B;
   if (gx > a.T) gx = a.T;
   const int tasks = 2 * a.n_kv + a.n_q;
-  int gy = (int)((2ll * sms + gx - 1) / gx);
+  int gy = (int)((4ll * sms + gx - 1) / gx);
   if (gy > (tasks + AP_WARPS - 1) / AP_WARPS) gy = (tasks + AP_WARPS - 1) / AP_WARPS;
   const size_t smem = (size_t)a.block * (tab.rot / 2) * sizeof(float2);   // at most 32 KiB
   const dim3 grid((unsigned)gx, (unsigned)gy);
-  if (head_dim == 128) return launch_k(append_kernel<T, 128>, grid, dim3(AP_THREADS), smem, st, false, a, tab, packed ? 1 : 0);
-  return launch_k(append_kernel<T, 64>, grid, dim3(AP_THREADS), smem, st, false, a, tab, packed ? 1 : 0);
+  if (head_dim == 128) return launch_k(append_kernel<T, 128>, grid, dim3(AP_THREADS), smem, st, true, a, tab, packed ? 1 : 0);
+  return launch_k(append_kernel<T, 64>, grid, dim3(AP_THREADS), smem, st, true, a, tab, packed ? 1 : 0);
 }
 
 }  // namespace
@@ -250,8 +283,7 @@ extern "C" int corun_kv8_append(const corun_kv8_cache *cache, const corun_kv8_ro
   if (rope && (!positions || rope->t.rot > cache->head_dim)) return CORUN_EINVAL;
   if (rows->T == 0) return CORUN_OK;
   int dev = 0, sms = 0;
-  cudaError_t ce = cudaGetDevice(&dev);
-  if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  cudaError_t ce = device_sms(&dev, &sms);
   if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   const corun_heads none{nullptr, 0, 0}, &qi = q ? *q : none, &qo = q ? *q_out : none;
   const AppendArgs a{(uint8_t *)cache->pool, cache->exps, cache->pages, cache->block, cache->n_kv, q ? n_q : 0, rows->B, rows->T, rows->max_blocks,

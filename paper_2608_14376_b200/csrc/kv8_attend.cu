@@ -566,8 +566,15 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         }
         if (sc) {
 #pragma unroll
-          for (int c = 0; c < C; ++c)
-            if (c < cols) sc[c] = y[c];
+          for (int c = 0; c < C; c += 4) {
+            if ((a.cols & 3) == 0) {
+              if (c < cols) *reinterpret_cast<float4 *>(sc + c) = make_float4(y[c], y[c + 1], y[c + 2], y[c + 3]);   // (a column behind the row's own is not read)
+            } else {
+#pragma unroll
+              for (int e = c; e < c + 4; ++e)
+                if (e < cols) sc[e] = y[e];
+            }
+          }
         }
         // the tile's frame: the largest s + e_v of every column
         float (*xm)[4] = sm.x_max[grp][k & 1];
@@ -813,12 +820,27 @@ __global__ void __launch_bounds__(256) attend_mass_kernel(const __grid_constant_
   const float *sc = a.scores + (long long)blockIdx.x * a.score_tokens * a.cols;
   float *mass = a.mass + (long long)blockIdx.x * a.max_blocks * a.block;
   for (int j = r.t_lo * AT_T + blockIdx.y * 256 + threadIdx.x; j < r.c; j += gridDim.y * 256) {
+    const float before = mass[j];
+    const float *sj = sc + (long long)j * a.cols;
     float sum = 0.f;
-    for (int c = 0; c < cols; ++c) {
-      const float2 f = ml[c];
-      sum = fmaf(ex2(__ldcg(sc + (long long)j * a.cols + c) - f.x), f.y, sum);
+    if ((a.cols & 3) == 0) {
+      for (int c = 0; c < cols; c += 4) {
+        const float4 s = __ldcg(reinterpret_cast<const float4 *>(sj + c));
+        const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < cols) {
+            const float2 f = ml[c + e];
+            sum = fmaf(ex2(v[e] - f.x), f.y, sum);
+          }
+      }
+    } else {
+      for (int c = 0; c < cols; ++c) {
+        const float2 f = ml[c];
+        sum = fmaf(ex2(__ldcg(sj + c) - f.x), f.y, sum);
+      }
     }
-    mass[j] += sum;
+    mass[j] = before + sum;
   }
 }
 
@@ -862,7 +884,7 @@ cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev,
     ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, a.cols), dim3(32 * AT_QUARTERS), 0, st, true, a);
   }
   if (ce == cudaSuccess && a.mass) {
-    int gy = (4 * sms + a.B * a.n_kv - 1) / (a.B * a.n_kv);
+    int gy = (16 * sms + a.B * a.n_kv - 1) / (a.B * a.n_kv);
     const long long most = (a.score_tokens + 255) / 256;
     if (gy > most) gy = (int)most;
     ce = launch_k(attend_mass_kernel, dim3(a.B * a.n_kv, gy), dim3(256), 0, st, true, a);
@@ -905,8 +927,7 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
   const AttendSpace s = attend_space(rows->B, max_new, n_q, cache->n_kv, cache->head_dim, cache->block, rows->max_blocks, mass != nullptr);
   if (ws_bytes < s.bytes) return CORUN_EINVAL;
   int dev = 0, sms = 0;
-  cudaError_t ce = cudaGetDevice(&dev);
-  if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  cudaError_t ce = device_sms(&dev, &sms);
   if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   CUtensorMap tm;
   int rc = tma_encode_kv8(&tm, cache->pool, (unsigned long long)cache->pages, cache->n_kv, cache->block, cache->head_dim, 2);

@@ -5,6 +5,7 @@
 // computes their cos and sin once into shared memory and uses them for all of its heads.
 #include <math.h>
 
+#include <atomic>
 #include <new>
 
 #include "kv8.cuh"
@@ -121,6 +122,17 @@ cudaError_t launch_rope(const RopeTable &tab, const HeadsView &v, bool wide, con
 }
 
 }  // namespace
+
+cudaError_t device_sms(int *dev, int *sms) {
+  static std::atomic<int> known[64];
+  cudaError_t ce = cudaGetDevice(dev);
+  if (ce != cudaSuccess) return ce;
+  if (*dev < 64 && (*sms = known[*dev].load(std::memory_order_relaxed)) > 0) return ce;
+  ce = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
+  if (ce == cudaSuccess && *dev < 64) known[*dev].store(*sms, std::memory_order_relaxed);
+  return ce;
+}
+
 }  // namespace corun
 
 using namespace corun;
@@ -182,8 +194,7 @@ int corun_rope_apply(const corun_rope *r, const corun_heads *x, const corun_head
   if (x->p == y->p && (x->token_stride != y->token_stride || x->head_stride != y->head_stride)) return CORUN_EINVAL;
   if (T == 0) return CORUN_OK;
   int dev = 0, sms = 0;
-  cudaError_t ce = cudaGetDevice(&dev);
-  if (ce == cudaSuccess) ce = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  cudaError_t ce = device_sms(&dev, &sms);
   if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   const int vec = 16 / (int)sz;
   const bool wide = heads_on_16(*x, dtype) && heads_on_16(*y, dtype) && head_dim % vec == 0 && r->t.rot % (r->t.interleaved ? vec : 2 * vec) == 0;
