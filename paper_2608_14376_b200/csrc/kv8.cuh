@@ -90,6 +90,55 @@ __device__ __forceinline__ float2 rope_cs(const RopeTable &tab, int pair, int po
   sincospif(hi, &s, &c);
   return make_float2(fmaf(-s, r, c) * tab.magnitude, fmaf(c, r, s) * tab.magnitude);
 }
+
+// x1 c - x2 s and x2 c + x1 s, rounded the same way in every kernel.
+__device__ __forceinline__ float turn1(float x1, float x2, float2 cs) { return fmaf(x1, cs.x, -__fmul_rn(x2, cs.y)); }
+__device__ __forceinline__ float turn2(float x1, float x2, float2 cs) { return fmaf(x2, cs.x, __fmul_rn(x1, cs.y)); }
+
+// A head cut into pieces of two groups of VEC values (16 bytes each): piece p of the rotated part holds VEC pairs, p VEC .. p VEC + VEC - 1; the
+// pieces behind it are the values that are not rotated.  Needs rot / 2 and head_dim / 2 to be multiples of VEC.
+template <typename T> struct Piece {
+  static constexpr int VEC = 16 / (int)sizeof(T);
+  alignas(16) T a[VEC], b[VEC];
+};
+struct PieceAt { int a, b; bool turned; };
+template <int VEC>
+__device__ __forceinline__ PieceAt piece_at(const RopeTable &tab, int p) {
+  const int half = tab.rot >> 1, n = half / VEC;
+  if (p >= n) { const int d = tab.rot + (p - n) * 2 * VEC; return {d, d + VEC, false}; }
+  if (tab.interleaved) return {2 * p * VEC, 2 * p * VEC + VEC, true};
+  return {p * VEC, half + p * VEC, true};
+}
+template <typename T>
+__device__ __forceinline__ void piece_load(Piece<T> &v, const T *x, const PieceAt &at) {
+  *reinterpret_cast<uint4 *>(v.a) = *reinterpret_cast<const uint4 *>(x + at.a);
+  *reinterpret_cast<uint4 *>(v.b) = *reinterpret_cast<const uint4 *>(x + at.b);
+}
+// The piece's values in 32 bits, rotated where it belongs to the rotated part: cs[i] is pair p VEC + i's cos and sin.
+template <typename T, int VEC>
+__device__ __forceinline__ void piece_turn(const Piece<T> &v, const float2 (&cs)[VEC], bool turned, bool interleaved, float (&a)[VEC], float (&b)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) { a[i] = to_f32(v.a[i]); b[i] = to_f32(v.b[i]); }
+  if (!turned) return;
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) {
+      const float a1 = a[2 * i], a2 = a[2 * i + 1], b1 = b[2 * i], b2 = b[2 * i + 1];
+      const float2 f = cs[i], g = cs[VEC / 2 + i];
+      a[2 * i] = turn1(a1, a2, f);
+      a[2 * i + 1] = turn2(a1, a2, f);
+      b[2 * i] = turn1(b1, b2, g);
+      b[2 * i + 1] = turn2(b1, b2, g);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const float x1 = a[i], x2 = b[i];
+      a[i] = turn1(x1, x2, cs[i]);
+      b[i] = turn2(x1, x2, cs[i]);
+    }
+  }
+}
 #endif
 
 }  // namespace corun

@@ -3,9 +3,9 @@
 // A unit is one page that a row's new tokens touch.  Its scale is set by all tokens of the page together, so one warp takes
 // a (page, key head, kind): it reads its tokens, finds the largest magnitude, settles the page's exponent, moves what the
 // page held before to it where it grew, and reads its tokens once more (from L1 by then) to store them.  The op is bound by
-// bytes (16-bit inputs in, a byte a value out, queries in and out); cos and sin, which cost some 100 instructions a pair, are
-// computed once per CTA and used for all of its heads.  Units are found from ctx and cu on the device: the launch's shape
-// depends on T and B alone, so it can be captured and replayed with other lengths.
+// bytes (16-bit inputs in, a byte a value out, queries in and out); cos and sin are computed once per CTA and used for all of
+// its heads.  Units are found from ctx and cu on the device: the launch's shape depends on T and B alone, so it can be captured
+// and replayed with other lengths.
 #include "kv8.cuh"
 
 namespace corun {
@@ -41,18 +41,14 @@ __device__ __forceinline__ int row_tokens(const int *ctx, const int *cu, int b, 
 
 // EPL neighbouring values of a head per lane: d0 = lane * EPL.
 template <typename T, int EPL>
-struct alignas(sizeof(T) * EPL) LanePack { T v[EPL]; };
+struct LanePack { T v[EPL]; };
 
 template <typename T, int EPL>
-__device__ __forceinline__ LanePack<T, EPL> lane_load(const T *x, bool packed) {
+__device__ __forceinline__ LanePack<T, EPL> lane_load(const T *x) {
   const int d0 = (threadIdx.x & 31) * EPL;
   LanePack<T, EPL> p;
-  if (packed) {
-    p = *reinterpret_cast<const LanePack<T, EPL> *>(x + d0);
-  } else {
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) p.v[e] = x[d0 + e];
-  }
+  for (int e = 0; e < EPL; ++e) p.v[e] = x[d0 + e];
   return p;
 }
 
@@ -69,8 +65,8 @@ __device__ __forceinline__ void lane_values(const LanePack<T, EPL> &p, const T *
       if (d0 + e < rot) {
         const float2 f = cs[(d0 + e) >> 1];
         const float x1 = o[e], x2 = o[e + 1];
-        o[e] = x1 * f.x - x2 * f.y;
-        o[e + 1] = x2 * f.x + x1 * f.y;
+        o[e] = turn1(x1, x2, f);
+        o[e + 1] = turn2(x1, x2, f);
       }
     }
     return;
@@ -87,8 +83,8 @@ __device__ __forceinline__ void lane_values(const LanePack<T, EPL> &p, const T *
       other = d < rot ? to_f32(x[d < half ? d + half : d - half]) : 0.f;
     }
     // (with shuffles o[e] is replaced below only after every lane has read it: one e at a time, and e is its own value)
-    if (d < half) o[e] = o[e] * cs[d].x - other * cs[d].y;
-    else if (d < rot) o[e] = o[e] * cs[d - half].x + other * cs[d - half].y;
+    if (d < half) o[e] = turn1(o[e], other, cs[d]);
+    else if (d < rot) o[e] = turn2(other, o[e], cs[d - half]);
   }
 }
 
@@ -101,21 +97,14 @@ __device__ __forceinline__ void store8(uint8_t *dst, const float (&x)[EPL], floa
   }
 }
 
-// AHEAD tokens of a head are requested together (16 at a time make the code so long that a CTA spends its time fetching it: a step of 64
-// rows took 17.6 us instead of 6).
-template <typename T, int HD>
-__global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTable tab,
-                                                            int packed) {
-  constexpr int EPL = HD / 32, AHEAD = 4;
-  typedef LanePack<T, EPL> P;
-  extern __shared__ float2 cs[];                  // [tokens of the unit][rot / 2]
-  __shared__ int s_warp[AP_WARPS], s_row, s_page, s_first, s_ctx, s_n;
+// The unit of this CTA (blockIdx.x): a row and one of the pages that its new tokens touch; units are numbered row by row.
+struct Unit { int row, page, first, c, n; };   // row -1: none (the grid is an upper bound)
+__device__ __forceinline__ Unit find_unit(const AppendArgs &a, int *s_warp, Unit *s_unit) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long reach = (long long)a.max_blocks * a.block;
-  if (tid == 0) s_row = -1;
+  if (tid == 0) s_unit->row = -1;
   griddep_wait();
   griddep_launch_dependents();
-  // which row and which of its pages: units are numbered row by row
   int before = 0;
   for (int b0 = 0; b0 < a.B; b0 += AP_THREADS) {
     const int b = b0 + tid;
@@ -135,20 +124,54 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
     int ahead = before, all = 0;
     for (int w = 0; w < AP_WARPS; ++w) { if (w < warp) ahead += s_warp[w]; all += s_warp[w]; }
     const int lo = ahead + inc - units;
-    if ((int)blockIdx.x >= lo && (int)blockIdx.x < lo + units) {
-      s_row = b;
-      s_page = (c - n) / a.block + (int)blockIdx.x - lo;
-      s_first = first; s_ctx = c; s_n = n;
-    }
+    if ((int)blockIdx.x >= lo && (int)blockIdx.x < lo + units) *s_unit = Unit{b, (c - n) / a.block + (int)blockIdx.x - lo, first, c, n};
     before += all;
     __syncthreads();
-    if (s_row >= 0) break;
+    if (s_unit->row >= 0) break;
   }
-  const int row = s_row;
-  if (row < 0) return;
-  const int jb = s_page, start = s_ctx - s_n;
-  const int z0 = max(0, start - jb * a.block), z1 = min(a.block, s_ctx - jb * a.block);   // the page's new tokens
-  const int t0 = s_first + jb * a.block + z0 - start, nt = z1 - z0;
+  return *s_unit;
+}
+
+// The exponent of a page that new tokens of largest magnitude mx come to, and what it held before moved to it (by a warp).
+template <int HD>
+__device__ __forceinline__ int settle(const AppendArgs &a, long long at, int z0, float mx) {
+  const int lane = threadIdx.x & 31;
+  int e = kv8_exp_of(mx);
+  if (z0 > 0) {
+    const int e_old = a.exps[at];
+    if (e > e_old) {
+      const float f = pow2f(max(e_old - e, -100));
+      uint4 *old = reinterpret_cast<uint4 *>(a.pool + at * a.block * HD);
+#pragma unroll 2
+      for (int i = lane; i < z0 * HD / 16; i += 32) {
+        uint4 x = old[i];
+        x.x = e4m3x4_shift(x.x, f); x.y = e4m3x4_shift(x.y, f); x.z = e4m3x4_shift(x.z, f); x.w = e4m3x4_shift(x.w, f);
+        old[i] = x;
+      }
+    } else {
+      e = e_old;
+    }
+  }
+  __syncwarp();
+  if (lane == 0) a.exps[at] = (int8_t)e;
+  return e;
+}
+
+// Value by value, for layouts whose heads do not start on 16 bytes or whose rotated part is not made of whole pieces.
+template <typename T, int HD>
+__global__ void __launch_bounds__(AP_THREADS) append_odd_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTable tab) {
+  constexpr int EPL = HD / 32, AHEAD = 4;
+  typedef LanePack<T, EPL> P;
+  extern __shared__ __align__(16) float2 cs[];                 // [tokens of the unit][rot / 2]
+  __shared__ int s_warp[AP_WARPS];
+  __shared__ Unit s_unit;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const Unit u = find_unit(a, s_warp, &s_unit);
+  if (u.row < 0) return;
+  const int row = u.row, jb = u.page, start = u.c - u.n;
+  const int z0 = max(0, start - jb * a.block), z1 = min(a.block, u.c - jb * a.block);   // the page's new tokens
+  const int t0 = u.first + jb * a.block + z0 - start, nt = z1 - z0;
+  const long long reach = (long long)a.max_blocks * a.block;
   const int pairs = tab.rot >> 1;
   for (int i = tid; i < nt * pairs; i += AP_THREADS) {
     const int t = i / pairs, p = i - t * pairs;
@@ -174,7 +197,7 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
       auto request = [&](int t1) {
 #pragma unroll
         for (int t = 0; t < AHEAD; ++t)
-          if (t1 + t < nt) raw[t] = lane_load<T, EPL>(x + (t1 + t) * step, packed);
+          if (t1 + t < nt) raw[t] = lane_load<T, EPL>(x + (t1 + t) * step);
       };
       for (int t1 = 0; t1 < nt; t1 += AHEAD) {
         request(t1);
@@ -189,28 +212,7 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-      int e_new = kv8_exp_of(mx);
-      if (z0 > 0) {
-        const int e_old = a.exps[at];
-        if (e_new > e_old) {                      // the tokens that are there already move to the larger scale
-          const float f = pow2f(max(e_old - e_new, -100));
-#pragma unroll 4
-          for (int t = 0; t < z0; ++t) {
-            if (EPL == 4) {
-              uint32_t *w = reinterpret_cast<uint32_t *>(dst + t * HD);
-              *w = e4m3x4_shift(*w, f);
-            } else {
-              uint16_t *w = reinterpret_cast<uint16_t *>(dst + t * HD);
-              const float2 v = e4m3x2_to(*w);
-              *w = (uint16_t)e4m3x2_of(v.x * f, v.y * f);
-            }
-          }
-        } else {
-          e_new = e_old;
-        }
-      }
-      __syncwarp();
-      if (lane == 0) a.exps[at] = (int8_t)e_new;
+      const int e_new = settle<HD>(a, at, z0, mx);
       const float f = pow2f(-e_new);
       for (int t1 = 0; t1 < nt; t1 += AHEAD) {
         if (nt > AHEAD) request(t1);
@@ -230,7 +232,7 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
         P raw[AHEAD];
 #pragma unroll
         for (int t = 0; t < AHEAD; ++t)
-          if (t1 + t < nt) raw[t] = lane_load<T, EPL>(x + (t1 + t) * a.q_t, packed);
+          if (t1 + t < nt) raw[t] = lane_load<T, EPL>(x + (t1 + t) * a.q_t);
 #pragma unroll
         for (int t = 0; t < AHEAD; ++t)
           if (t1 + t < nt) {
@@ -238,23 +240,142 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
             lane_values<T, EPL>(raw[t], x + (t1 + t) * a.q_t, cs + (t1 + t) * pairs, tab.rot, tab.interleaved, o);
             __syncwarp();                           // (in place: every partner has been read)
             T *to = y + (t1 + t) * a.o_t + lane * EPL;
-            P p;
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) p.v[e] = from_f32<T>(o[e]);
-            if (packed) {
-              *reinterpret_cast<P *>(to) = p;
-            } else {
-#pragma unroll
-              for (int e = 0; e < EPL; ++e) to[e] = p.v[e];
-            }
+            for (int e = 0; e < EPL; ++e) to[e] = from_f32<T>(o[e]);
           }
       }
     }
   }
 }
 
+// Sixteen bytes at a time: a thread holds a piece of a head (two groups of VEC values that are rotated together).  Keys and values: a
+// warp per (kind, head), NP lanes a token, so 4 (fp32: 2; heads of 64: twice that) tokens at a time, twice over the page's new tokens.
+// Queries: a thread per (token, piece) goes through heads with its pairs' cos and sin in registers.
+template <typename T, int HD>
+__global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTable tab) {
+  constexpr int VEC = Piece<T>::VEC, NP = HD / (2 * VEC), SLOTS = AP_THREADS / NP, STEP = 32 / NP, AHEAD = 4;
+  extern __shared__ __align__(16) float2 cs_s[];              // [tokens of the unit][rot / 2]
+  __shared__ int s_warp[AP_WARPS];
+  __shared__ Unit s_unit;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const Unit u = find_unit(a, s_warp, &s_unit);
+  if (u.row < 0) return;
+  const int jb = u.page, start = u.c - u.n;
+  const int z0 = max(0, start - jb * a.block), z1 = min(a.block, u.c - jb * a.block);   // the page's new tokens
+  const int t0 = u.first + jb * a.block + z0 - start, nt = z1 - z0;
+  const int pairs = tab.rot >> 1;
+  for (int i = tid; i < nt * pairs; i += AP_THREADS) {
+    const int t = i / pairs, p = i - t * pairs;
+    cs_s[i] = rope_cs(tab, p, __ldg(a.positions + t0 + t));
+  }
+  __syncthreads();
+  const int piece = tid % NP;
+  const PieceAt at = piece_at<VEC>(tab, piece);
+  auto angles = [&](int t, float2 (&cs)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 2) {
+      const float4 f = *reinterpret_cast<const float4 *>(cs_s + t * pairs + piece * VEC + i);
+      cs[i] = make_float2(f.x, f.y);
+      cs[i + 1] = make_float2(f.z, f.w);
+    }
+  };
+  const long long page = __ldg(a.block_table + (long long)u.row * a.max_blocks + jb);
+  const bool page_ok = page >= 0 && page < a.pages;
+  for (int task = blockIdx.y * AP_WARPS + warp; task < 2 * a.n_kv; task += gridDim.y * AP_WARPS) {
+    const int kind = task & 1, h = task >> 1;
+    if (kind == 0 && a.mass) {
+      const long long reach = (long long)a.max_blocks * a.block;
+      for (int i = lane; i < nt; i += 32) a.mass[((long long)u.row * a.n_kv + h) * reach + (long long)jb * a.block + z0 + i] = 0.f;
+    }
+    if (!page_ok) continue;
+    const long long step = kind ? a.v_t : a.k_t;
+    const T *x = (const T *)(kind ? a.v : a.k) + (long long)t0 * step + (long long)h * (kind ? a.v_h : a.k_h);
+    const bool turned = kind == 0 && at.turned;
+    const long long block_at = (page * 2 + kind) * a.n_kv + h;
+    uint8_t *dst = a.pool + (block_at * a.block + z0) * HD;
+    float mx = 0.f;
+    // AHEAD tokens of a lane are requested together; with no more than that they are kept for the second time
+    Piece<T> v[AHEAD];
+    auto request = [&](int tb) {
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (tb + e * STEP < nt) piece_load(v[e], x + (tb + e * STEP) * step, at);
+    };
+    for (int tb = lane / NP; tb < nt; tb += AHEAD * STEP) {
+      request(tb);
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (tb + e * STEP < nt) {
+          float2 cs[VEC];
+          float p[VEC], q[VEC];
+          if (turned) angles(tb + e * STEP, cs);
+          piece_turn(v[e], cs, turned, tab.interleaved, p, q);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) mx = fmaxf(mx, fmaxf(fabsf(p[i]), fabsf(q[i])));
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float f = pow2f(-settle<HD>(a, block_at, z0, mx));
+    for (int tb = lane / NP; tb < nt; tb += AHEAD * STEP) {
+      if (nt > AHEAD * STEP) request(tb);
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (tb + e * STEP < nt) {
+          const int t = tb + e * STEP;
+          float2 cs[VEC];
+          float p[VEC], q[VEC];
+          if (turned) angles(t, cs);
+          piece_turn(v[e], cs, turned, tab.interleaved, p, q);
+          uint32_t w[2][VEC / 4];
+#pragma unroll
+          for (int i = 0; i < VEC; i += 4) {
+            w[0][i / 4] = e4m3x2_of(p[i] * f, p[i + 1] * f) | (e4m3x2_of(p[i + 2] * f, p[i + 3] * f) << 16);
+            w[1][i / 4] = e4m3x2_of(q[i] * f, q[i + 1] * f) | (e4m3x2_of(q[i + 2] * f, q[i + 3] * f) << 16);
+          }
+          if (VEC == 8) {
+            *reinterpret_cast<uint2 *>(dst + t * HD + at.a) = make_uint2(w[0][0], w[0][VEC / 4 - 1]);
+            *reinterpret_cast<uint2 *>(dst + t * HD + at.b) = make_uint2(w[1][0], w[1][VEC / 4 - 1]);
+          } else {
+            *reinterpret_cast<uint32_t *>(dst + t * HD + at.a) = w[0][0];
+            *reinterpret_cast<uint32_t *>(dst + t * HD + at.b) = w[1][0];
+          }
+        }
+    }
+  }
+  // queries: the slots are shared out among tokens (a power of two of them) and heads
+  if (a.n_q == 0) return;
+  int ts = 0;
+  while ((1 << ts) < nt && (1 << ts) < SLOTS) ++ts;
+  const int slot = tid / NP, heads_at_once = SLOTS >> ts;
+  const int per = (a.n_q + gridDim.y - 1) / gridDim.y, h0 = blockIdx.y * per, h1 = min(a.n_q, h0 + per);
+  for (int t = slot & ((1 << ts) - 1); t < nt; t += 1 << ts) {
+    float2 cs[VEC];
+    if (at.turned) angles(t, cs);
+    const T *x = (const T *)a.q + (long long)(t0 + t) * a.q_t;
+    T *y = (T *)a.q_out + (long long)(t0 + t) * a.o_t;
+    for (int hb = h0 + (slot >> ts); hb < h1; hb += AHEAD * heads_at_once) {
+      Piece<T> v[AHEAD];
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (hb + e * heads_at_once < h1) piece_load(v[e], x + (long long)(hb + e * heads_at_once) * a.q_h, at);
+#pragma unroll
+      for (int e = 0; e < AHEAD; ++e)
+        if (hb + e * heads_at_once < h1) {
+          float p[VEC], q[VEC];
+          piece_turn(v[e], cs, at.turned, tab.interleaved, p, q);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) { v[e].a[i] = from_f32<T>(p[i]); v[e].b[i] = from_f32<T>(q[i]); }
+          T *to = y + (long long)(hb + e * heads_at_once) * a.o_h;
+          *reinterpret_cast<uint4 *>(to + at.a) = *reinterpret_cast<const uint4 *>(v[e].a);
+          *reinterpret_cast<uint4 *>(to + at.b) = *reinterpret_cast<const uint4 *>(v[e].b);
+        }
+    }
+  }
+}
+
 template <typename T>
-cudaError_t launch_append(const AppendArgs &a, const RopeTable &tab, int head_dim, bool packed, int sms, cudaStream_t st) {
+cudaError_t launch_append(const AppendArgs &a, const RopeTable &tab, int head_dim, bool wide, int sms, cudaStream_t st) {
   // a row's n tokens touch at most (n - 1) / block + 2 pages, and no more than n
   long long gx = (long long)a.T / a.block + 2ll * a.B;
   if (gx > a.T) gx = a.T;
@@ -263,8 +384,9 @@ cudaError_t launch_append(const AppendArgs &a, const RopeTable &tab, int head_di
   if (gy > (tasks + AP_WARPS - 1) / AP_WARPS) gy = (tasks + AP_WARPS - 1) / AP_WARPS;
   const size_t smem = (size_t)a.block * (tab.rot / 2) * sizeof(float2);   // at most 32 KiB
   const dim3 grid((unsigned)gx, (unsigned)gy);
-  if (head_dim == 128) return launch_k(append_kernel<T, 128>, grid, dim3(AP_THREADS), smem, st, true, a, tab, packed ? 1 : 0);
-  return launch_k(append_kernel<T, 64>, grid, dim3(AP_THREADS), smem, st, true, a, tab, packed ? 1 : 0);
+  void (*kernel)(const AppendArgs, const RopeTable) =
+      wide ? (head_dim == 128 ? append_kernel<T, 128> : append_kernel<T, 64>) : (head_dim == 128 ? append_odd_kernel<T, 128> : append_odd_kernel<T, 64>);
+  return launch_k(kernel, grid, dim3(AP_THREADS), smem, st, true, a, tab);
 }
 
 }  // namespace
@@ -291,12 +413,12 @@ extern "C" int corun_kv8_append(const corun_kv8_cache *cache, const corun_kv8_ro
                      v->token_stride, v->head_stride, qi.token_stride, qi.head_stride, qo.token_stride, qo.head_stride, mass};
   static const RopeTable still = {};               // rot 0: nothing is rotated
   const RopeTable &tab = rope ? rope->t : still;
-  // a lane's values (2 or 4) in one load or store where every head starts on 16 bytes
-  const bool packed = heads_on_16(*k, dtype) && heads_on_16(*v, dtype) && (!q || (heads_on_16(qi, dtype) && heads_on_16(qo, dtype)));
+  const bool wide = heads_on_16(*k, dtype) && heads_on_16(*v, dtype) && (!q || (heads_on_16(qi, dtype) && heads_on_16(qo, dtype))) &&
+                    tab.rot / 2 % (16 / (int)sz) == 0;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (dtype == CORUN_F32) ce = launch_append<float>(a, tab, cache->head_dim, packed, sms, st);
-  else if (dtype == CORUN_BF16) ce = launch_append<__nv_bfloat16>(a, tab, cache->head_dim, packed, sms, st);
-  else ce = launch_append<__half>(a, tab, cache->head_dim, packed, sms, st);
+  if (dtype == CORUN_F32) ce = launch_append<float>(a, tab, cache->head_dim, wide, sms, st);
+  else if (dtype == CORUN_BF16) ce = launch_append<__nv_bfloat16>(a, tab, cache->head_dim, wide, sms, st);
+  else ce = launch_append<__half>(a, tab, cache->head_dim, wide, sms, st);
   if (ce != cudaSuccess) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
   return CORUN_OK;
 }
