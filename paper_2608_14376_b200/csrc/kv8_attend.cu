@@ -225,7 +225,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       all += sm.warp_items[w];
       call += sm.warp_cost[w];
     }
-    if (all == 0) griddep_launch_dependents();        // nothing to do here: the kernel for the other rows may begin
     if (tid < a.B) sm.row_item[tid] = inc;
     if (tid == 0) sm.row_item[a.B] = all;
     // a CTA's stretch: from the first item that starts at or behind blockIdx / gridDim of all cost, to the next CTA's
@@ -245,6 +244,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
       sm.mine.acc = (rest * split) % ns;
     }
   }
+  // the next kernel's blocks may come up beside this one's and wait for its end (all CTAs of this grid run at once)
+  griddep_launch_dependents();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -735,25 +736,26 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
   if (warp == 0) tmem_dealloc(s_tmem, TMEM_COLS);
 }
 
-// One block per (row, key head, column): each of four warps takes a quarter of the row's splits, ascending, hd / 32 dims a lane; the quarters
-// are added in their order.
-constexpr int AT_QUARTERS = 4;
+// One block per (row, key head, column): each of four warps (eight for rows with more than AT_MANY splits) takes a part of the row's splits,
+// ascending, hd / 32 dims a lane; the parts are added in their order.
+constexpr int AT_PARTS = 8, AT_MANY = 32;
 template <int W> struct alignas(4 * W) Floats { float v[W]; };
 template <typename T, int HD>
-__global__ void __launch_bounds__(32 * AT_QUARTERS) attend_combine_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(32 * AT_PARTS) attend_combine_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int W = HD / 32, AHEAD = 8;
   typedef Floats<W> F;
   griddep_launch_dependents();
   __shared__ float2 sml[AT_SPLITS];
-  __shared__ F so[AT_QUARTERS][32];
-  __shared__ float sl[AT_QUARTERS];
+  __shared__ F so[AT_PARTS][32];
+  __shared__ float sl[AT_PARTS];
   const int b = blockIdx.x / a.n_kv, g = blockIdx.x - b * a.n_kv, col = blockIdx.y, q = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.n_q / a.n_kv;
   const int first = a.cu ? a.cu[b] : b, end = a.cu ? a.cu[b + 1] : b + 1;
   const RowPlan r = row_plan(a.ctx[b], first, end, a, G);
   griddep_wait();
   if (r.ns <= 1 || col >= r.n * G) return;
   const long long at = (long long)blockIdx.x * a.max_splits;
-  const int per = (r.ns + AT_QUARTERS - 1) / AT_QUARTERS, lo = q * per, hi = min(r.ns, lo + per);
+  const int parts = r.ns > AT_MANY ? AT_PARTS : AT_PARTS / 2;
+  const int per = (r.ns + parts - 1) / parts, lo = q * per, hi = min(r.ns, lo + per);
   const float *po = a.part_o + (at * a.cols + col) * HD + lane * W;
   const long long step = (long long)a.cols * HD;
   auto load = [&](int s) {
@@ -771,7 +773,7 @@ __global__ void __launch_bounds__(32 * AT_QUARTERS) attend_combine_kernel(const 
 #pragma unroll
   for (int e = 0; e < AHEAD; ++e)
     if (lo + e < hi) x[e] = load(lo + e);
-  for (int s = threadIdx.x; s < r.ns; s += 32 * AT_QUARTERS) sml[s] = __ldcg(a.part_ml + (at + s) * a.cols + col);
+  for (int s = threadIdx.x; s < r.ns; s += blockDim.x) sml[s] = __ldcg(a.part_ml + (at + s) * a.cols + col);
   __syncthreads();
   float M = AT_LOW;
   for (int s = lane; s < r.ns; s += 32) M = fmaxf(M, sml[s].x);
@@ -799,8 +801,7 @@ __global__ void __launch_bounds__(32 * AT_QUARTERS) attend_combine_kernel(const 
   if (d >= HD) return;
   float sum = 0.f;
   L = 0.f;
-#pragma unroll
-  for (int e = 0; e < AT_QUARTERS; ++e) { L += sl[e]; sum += so[e][d / W].v[d % W]; }
+  for (int e = 0; e < parts; ++e) { L += sl[e]; sum += so[e][d / W].v[d % W]; }
   const float inv = L > 0.f || L != L ? 1.f / L : 0.f;
   ((T *)a.out)[(long long)(first + col / G) * a.o_t + (long long)(g * G + col % G) * a.o_h + d] = from_f32<T>(sum * inv);
   if (a.mass && d == 0) a.ml[(long long)blockIdx.x * a.cols + col] = make_float2(M - 8.f, inv);
@@ -881,7 +882,7 @@ cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev,
   }
   ce = launch_k(attend_kernel<T, HD, C>, dim3(sms), dim3(AT_THREADS), smem, st, true, tm, a);
   if (ce == cudaSuccess && a.max_splits > 1) {
-    ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, a.cols), dim3(32 * AT_QUARTERS), 0, st, true, a);
+    ce = launch_k(attend_combine_kernel<T, HD>, dim3(a.B * a.n_kv, a.cols), dim3(32 * (a.max_splits > AT_MANY ? AT_PARTS : AT_PARTS / 2)), 0, st, true, a);
   }
   if (ce == cudaSuccess && a.mass) {
     int gy = (16 * sms + a.B * a.n_kv - 1) / (a.B * a.n_kv);
