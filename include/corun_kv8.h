@@ -69,7 +69,8 @@ int corun_kv8_append(const corun_kv8_cache *cache, const corun_kv8_rows *rows, c
  *   dtype     of q and out: CORUN_BF16 or CORUN_F16; heads start on 16 bytes
  *   max_new   largest number of new tokens of a row (cu NULL: 1); a row with more is left out
  *   ws        corun_kv8_attend_bytes(...) bytes, 256-byte aligned, the call's own until it has run
- * n_q a multiple of n_kv, n_q / n_kv <= 32, B <= 512, scale > 0.  Queries and softmax weights enter the tensor cores as
+ * A NaN among the values of a token reaches every query that sees the token, and may reach other queries of the same row and call.
+ * n_q a multiple of n_kv, n_q / n_kv <= 32, B <= 512, scale > 0, T / (128 / (n_q / n_kv)) + B at most some 65000 (EINVAL beyond).  Queries and softmax weights enter the tensor cores as
  * sums of e4m3 values that hold 11 or more bits of them; scores, weights' sums and outputs are held in 32 bits.
  * Errors: EINVAL, ECUDA.  A bounded device-side wait that expires is recorded in ws: corun_kv8_sync waits for the
  * stream and returns ETIMEOUT in that case.

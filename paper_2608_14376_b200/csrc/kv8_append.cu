@@ -27,12 +27,12 @@ struct AppendArgs {
 
 // New tokens of row b and the first of them, or 0 where the row is left out.
 __device__ __forceinline__ int row_tokens(const int *ctx, const int *cu, int b, int T, long long reach, int &first, int &c) {
-  c = __ldg(ctx + b);
+  c = __ldcg(ctx + b);
   int n = 1;
   first = b;
   if (cu) {
-    first = __ldg(cu + b);
-    const int end = __ldg(cu + b + 1);
+    first = __ldcg(cu + b);
+    const int end = __ldcg(cu + b + 1);
     n = end - first;
     if (first < 0 || end < first || end > T) return 0;
   }
@@ -175,10 +175,10 @@ __global__ void __launch_bounds__(AP_THREADS) append_odd_kernel(const __grid_con
   const int pairs = tab.rot >> 1;
   for (int i = tid; i < nt * pairs; i += AP_THREADS) {
     const int t = i / pairs, p = i - t * pairs;
-    cs[i] = rope_cs(tab, p, __ldg(a.positions + t0 + t));
+    cs[i] = rope_cs(tab, p, __ldcg(a.positions + t0 + t));
   }
   __syncthreads();
-  const long long page = __ldg(a.block_table + (long long)row * a.max_blocks + jb);
+  const long long page = __ldcg(a.block_table + (long long)row * a.max_blocks + jb);
   const bool page_ok = page >= 0 && page < a.pages;
   const int n_task = 2 * a.n_kv + a.n_q;
   for (int task = blockIdx.y * AP_WARPS + warp; task < n_task; task += gridDim.y * AP_WARPS) {
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
   const int pairs = tab.rot >> 1;
   for (int i = tid; i < nt * pairs; i += AP_THREADS) {
     const int t = i / pairs, p = i - t * pairs;
-    cs_s[i] = rope_cs(tab, p, __ldg(a.positions + t0 + t));
+    cs_s[i] = rope_cs(tab, p, __ldcg(a.positions + t0 + t));
   }
   __syncthreads();
   const int piece = tid % NP;
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(AP_THREADS) append_kernel(const __grid_constan
       cs[i + 1] = make_float2(f.z, f.w);
     }
   };
-  const long long page = __ldg(a.block_table + (long long)u.row * a.max_blocks + jb);
+  const long long page = __ldcg(a.block_table + (long long)u.row * a.max_blocks + jb);
   const bool page_ok = page >= 0 && page < a.pages;
   for (int task = blockIdx.y * AP_WARPS + warp; task < 2 * a.n_kv; task += gridDim.y * AP_WARPS) {
     const int kind = task & 1, h = task >> 1;

@@ -453,12 +453,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         const T *src = (const T *)a.q + (long long)(x.first + c / G) * a.q_t + (long long)(x.g * G + c % G) * a.q_h + lane * EPL;
         float v[EPL];
         if (EPL == 4) {
-          const uint2 u = __ldg(reinterpret_cast<const uint2 *>(src));
+          const uint2 u = __ldcg(reinterpret_cast<const uint2 *>(src));
           const T *e = reinterpret_cast<const T *>(&u);
 #pragma unroll
           for (int i = 0; i < EPL; ++i) v[i] = to_f32(e[i]);
         } else {
-          const uint32_t u = __ldg(reinterpret_cast<const uint32_t *>(src));
+          const uint32_t u = __ldcg(reinterpret_cast<const uint32_t *>(src));
           const T *e = reinterpret_cast<const T *>(&u);
 #pragma unroll
           for (int i = 0; i < EPL; ++i) v[i] = to_f32(e[i]);
@@ -874,6 +874,7 @@ cudaError_t launch_attend_c(const CUtensorMap &tm, const AttendArgs &a, int dev,
   // the shared-memory size is opted into once per device
   static std::atomic<uint64_t> done{0};
   constexpr int smem = smem_bytes<T, HD, C>();
+  static_assert(smem <= 232448, "shared memory of a CTA");
   cudaError_t ce = cudaSuccess;
   if (dev >= 64 || !(done.load() >> dev & 1)) {
     ce = cudaFuncSetAttribute(attend_kernel<T, HD, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -922,6 +923,7 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
   if (!kv8_cache_ok(cache) || !kv8_rows_ok(rows, cache) || !q || !out || !q->p || !out->p || (dtype != CORUN_BF16 && dtype != CORUN_F16) ||
       rows->B > AT_MAXB || max_new < 1 || (!rows->cu && max_new != 1) || n_q < 1 || n_q % cache->n_kv || n_q / cache->n_kv > AT_MAXC || !(scale > 0.f) || isinf(scale) ||
       window < 0 || (mass && (int64_t)max_new * (n_q / cache->n_kv) > AT_MAXC) || !heads_on_16(*q, dtype) || !heads_on_16(*out, dtype) || !ws ||
+      kv8_chunk_tiles(rows->T, rows->B, n_q / cache->n_kv) > 65535 ||
       !aligned_to(ws, 256))
     return CORUN_EINVAL;
   if (rows->T == 0) return CORUN_OK;

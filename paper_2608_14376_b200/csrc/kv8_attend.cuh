@@ -34,7 +34,7 @@ struct AttendArgs {
 // Whether a row of the call takes part.
 __device__ __forceinline__ bool at_row_ok(int c, int first, int end, const AttendArgs &a) {
   const int n = end - first;
-  return c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && n > 0 && n <= a.max_new && end <= a.T;
+  return c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && end > first && n <= a.max_new && end <= a.T;
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -58,19 +58,27 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Loads that are issued where they stand (the compiler may move an ordinary one down to its first use).
+// Loads that are issued where they stand (the compiler may move an ordinary one down to its first use), from L2: this kernel may have come up
+// beside the one that wrote the values, whose SM-local lines a cached load could still meet.
 __device__ __forceinline__ int load_now(const int *p) {
   int v;
-  asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(v) : "l"(p));
+  asm volatile("ld.global.cg.b32 %0, [%1];" : "=r"(v) : "l"(p));
   return v;
 }
 __device__ __forceinline__ int load_now(const int8_t *p) {
   int v;
-  asm volatile("ld.global.nc.s8 %0, [%1];" : "=r"(v) : "l"(p));
+  asm volatile("ld.global.cg.s8 %0, [%1];" : "=r"(v) : "l"(p));
   return v;
 }
 #endif
 
+// Tiles that the new tokens of a call's rows with more than AT_MAXC columns can make at most: a row's n tokens are n / TQ + 1 or fewer, and
+// rows with AT_MAXC columns or fewer have none.
+inline long long kv8_chunk_tiles(int T, int B, int G) {
+  const int least = AT_MAXC / G + 1;
+  const long long rows = T / least < B ? T / least : B;
+  return T / (128 / G) + rows;
+}
 // Rows with more than AT_MAXC columns.  tm: tensor map whose boxes hold one page of one head and kind.  dtype: CORUN_BF16 or CORUN_F16.
 cudaError_t launch_kv8_chunk(const CUtensorMap &tm, const AttendArgs &a, int head_dim, int dtype, int dev, cudaStream_t st);
 

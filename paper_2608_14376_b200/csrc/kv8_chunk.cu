@@ -15,7 +15,10 @@
 // A query row is brought to [256, 512) by a power of two before it is rounded to fp16: exact for bf16, and for fp16, but for values
 // some 2^-22 of the row's largest.
 //
-// Measured on 3 rows of 277, 553 and 521 new tokens behind up to 8192 cached ones (32 query, 8 key heads of 128): CHUNK_FIGURES.
+// Measured on 3 rows of 200 to 700 new tokens behind up to 8192 cached ones (32 query, 8 key heads of 128, bf16): 247 us, 477 TFLOP/s; the
+// kernel for few columns took 1484.  A block takes 3300 to 3700 cycles, of which the products need 1024: the softmax (some 900 instructions a
+// warp and block, and a third of all issue slots), the output and the turning share the schedulers (62 % of issue slots, ALU pipe 42 %,
+// tensor pipe 27 %).  Turning with one fp16 tile of values and two of keys: 315 us; whichever product can go on first: 256.
 //
 // Every reduction has one fixed order that depends on the row's own lengths only.  All waits are bounded.
 #include <math_constants.h>
@@ -171,7 +174,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     for (int k = 0; k < 8 / RPW; ++k) {
       const int m = RPW * (warp + 16 * k) + lane / LPR, t = m / G;
       v[k] = make_uint2(0u, 0u);
-      if (t < n_tok) v[k] = __ldg(reinterpret_cast<const uint2 *>((const T *)a.q + (long long)(t_first + t) * a.q_t + (long long)(g * G + m % G) * a.q_h + d));
+      if (t < n_tok) v[k] = __ldcg(reinterpret_cast<const uint2 *>((const T *)a.q + (long long)(t_first + t) * a.q_t + (long long)(g * G + m % G) * a.q_h + d));
     }
 #pragma unroll
     for (int k = 0; k < 8 / RPW; ++k) {
@@ -436,12 +439,7 @@ cudaError_t launch_chunk(const CUtensorMap &tm, const AttendArgs &a, int dev, cu
     if (ce != cudaSuccess) return ce;
     if (dev < 64) done.fetch_or(1ull << dev);
   }
-  // a row's n tokens are at most n / TQ + 1 tiles, and rows with AT_MAXC columns or fewer have none
-  const int G = a.n_q / a.n_kv, TQ = 128 / G, least = AT_MAXC / G + 1;
-  long long rows = a.T / least;
-  if (rows > a.B) rows = a.B;
-  const long long tiles = a.T / TQ + rows;
-  if (tiles > 65535) return cudaErrorInvalidConfiguration;
+  const long long tiles = kv8_chunk_tiles(a.T, a.B, a.n_q / a.n_kv);
   return launch_k(chunk_kernel<T, HD>, dim3(a.n_kv, (unsigned)(tiles < 1 ? 1 : tiles)), dim3(CH_THREADS), smem, st, true, tm, a);
 }
 

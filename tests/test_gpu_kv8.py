@@ -533,3 +533,50 @@ def test_decode_with_eviction(torch, corun):
             slack[b, :, :ctx[b]] += (p[0] * (2.0 ** -16 * a[0][:, None] + 2.0 ** -21)).reshape(n_kv, G, -1).sum(1) + 2.0 ** -22 * total[b, :, :ctx[b]]
     for b in range(B):                                           # the prompt's tokens began at 0: append made them so
         assert np.all(np.abs(_np(mass)[b, :, :ctx[b]] - total[b, :, :ctx[b]]) <= slack[b, :, :ctx[b]])
+
+
+@pytest.mark.parametrize("n_kv,G,hd,dtype", [(2, 8, 128, "float16"), (1, 8, 64, "float16"), (2, 4, 128, "bfloat16"), (1, 12, 128, "float16")])
+def test_steps_replayed_from_a_graph(torch, corun, n_kv, G, hd, dtype):
+    """Append and attention one behind the other in one captured graph, replayed with new inputs and lengths: the bytes of separate
+    calls with a wait between them."""
+    dt, B, block = getattr(torch, dtype), 3, 16
+    s = Setup(torch, corun, [200, 31, 0], n_kv, hd, block, seed=G, spare_blocks=4)
+    other = corun.Kv8Cache(s.cache.pages, n_kv, hd, block, pool=s.cache.pool.clone(), exps=s.cache.exps.clone())
+    rope = corun.Rope(hd)
+    att = corun.Kv8Attention(B, G * n_kv, n_kv, hd, s.max_blocks, block)
+    mk = lambda h: torch.zeros(B, h, hd, dtype=dt, device="cuda")
+    q, k, v, q_out, out = mk(G * n_kv), mk(n_kv), mk(n_kv), mk(G * n_kv), mk(G * n_kv)
+    ctx, pos = _i32(torch, [200, 31, 0]), _i32(torch, [0, 0, 0])
+    mass, mass2 = (torch.zeros(B, n_kv, s.max_blocks * block, device="cuda") for _ in range(2))
+
+    def step(cache, mass, o, qo):
+        cache.append(k, v, ctx, s.t_table, positions=pos, rope=rope, q=q, q_out=qo, mass=mass)
+        return att.run(qo, cache, ctx, s.t_table, 0.05, mass=mass, out=o)
+
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(s.cache, mass, out, q_out)
+    for i in range(20):
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, device="cuda") * (4.0 ** (i % 4)))
+        ctx += (ctx > 0).int()
+        pos += 1
+        g.replay()
+        o2, q2 = torch.zeros_like(out), torch.zeros_like(q_out)
+        torch.cuda.synchronize()
+        other.append(k, v, ctx, s.t_table, positions=pos, rope=rope, q=q, q_out=q2, mass=mass2)
+        torch.cuda.synchronize()
+        att.run(q2, other, ctx, s.t_table, 0.05, mass=mass2, out=o2)
+        att.sync()
+        assert torch.equal(out[:2], o2[:2]) and torch.equal(q_out[:2], q2[:2]) and torch.equal(mass, mass2)
+        assert torch.equal(s.cache.exps, other.exps)
+    assert torch.equal(s.cache.pool.view(torch.uint8), other.pool.view(torch.uint8))
+    _check_attend(torch, Sub(s), q_out[:2], out[:2], None, None, ctx.tolist()[:2], [1, 1], 0, float(np.float32(0.05)))
+
+
+class Sub:
+    """The cache as it is now, for ``_check_attend``."""
+
+    def __init__(self, s):
+        self.table, self.n_kv, self.want = s.table, s.n_kv, ko.Cache(*s.state())
