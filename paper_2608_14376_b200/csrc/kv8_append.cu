@@ -6,6 +6,8 @@
 // bytes (16-bit inputs in, a byte a value out, queries in and out); cos and sin are computed once per CTA and used for all of
 // its heads.  Units are found from ctx and cu on the device: the launch's shape depends on T and B alone, so it can be captured
 // and replayed with other lengths.
+// One token for each of 64 rows (32 query, 8 key heads of 128, bf16): 6 us, a chain of latencies (lengths, positions, keys, stores).  1252
+// tokens of 3 rows: 14.6 us (4.4 at the copy rate; some 80 pages, 128 registers a thread).
 #include "kv8.cuh"
 
 namespace corun {

@@ -2,30 +2,39 @@
 // received, on tcgen05 / TMEM / TMA (sm_100a) straight from the 8-bit pages.
 //
 // The cached tokens are the M side of both products and the query columns (query tokens x query heads of a key head, at most
-// 32 a tile) the N side, so that the cache's bytes are MMA operands as they lie in memory: no value of K or V passes
-// through a register.
-//   scores   S^T [128 tokens x 3 C] = K [128 x hd] * Q^T        K K-major, 32 values of a row per MMA
-//   output   O^T [hd x 3 C]         = V^T [hd x 128] * P^T      V read as the MN-major A operand
-// kind::f8f6f4 wants 8-bit operands on both sides.  A query (16 bits) or a weight (11 bits, fp16) is the sum of three e4m3
-// values, x = h0 + h1 / 16 + h2 / 256, each the rounding of what the ones before left (4 bits each: exact for 11 bits and
-// for bf16), and takes three columns; with few columns an MMA costs the same whatever N is, so the three are free.  Queries are
-// brought to [128, 256) by a power of two per column, weights to at most 256.
+// 32) the N side, so that the cache's bytes are MMA operands as they lie in memory: no value of K or V passes
+// through a register.  With C columns:
+//   scores   S^T [128 tokens x 2 or 3 C] = K [128 x hd] * Q^T   K K-major, 32 values of a row per MMA
+//   output   O^T [hd x 3 C]              = V^T [hd x 128] * P^T V read as the MN-major A operand
+// kind::f8f6f4 wants 8-bit operands on both sides.  A query or a weight is the sum of e4m3 values, x = h0 + h1 / 16 + h2 / 256, each
+// the rounding of what the ones before left (4 bits each), and takes a column for each: a bf16 query two (8 bits, exact), an fp16 query three
+// (11 bits, exact), a weight three (it is rounded to fp16's 11 bits first).  With few columns an MMA costs the same whatever N is, so they are
+// free.  Queries are brought to [128, 256) by a power of two per column, weights to at most 256.
 // The scales 2^e of a token's keys multiply its scores.  Those of its values go into its weight: the product takes
 // w = 2^(s + e_v - M), M the largest s + e_v of the column in the tile, so that what is rounded is rounded relative to its
-// share in the result; the sum of weights takes w 2^-e_v back.
+// share in the result; the sum of weights takes w 2^-e_v back.  (Exponents lie in [-32, 31]: neither leaves the range of 32 bits.)
 // A tile's output stays in its own frame M; it is added to the running output, held in registers, in 32 bits.
 //
-// An item is (row, tile of query columns, key head, split).  Rows with n G <= 32 columns are split into parts (at_splits); rows with
-// more columns are kv8_chunk.cu's.  The split depends on the row's own ctx, n and window alone, sums
-// have one fixed order, and which CTA computes an item has no influence on any value: a row's result does not depend on
-// the other rows.  Every CTA (one per SM) takes a stretch of the item list, cut by cost.
+// An item is (row, key head, split).  Rows with n G <= 32 columns are split into parts (at_splits); rows with more columns are
+// kv8_chunk.cu's.  The split depends on the row's own ctx, n and window alone, sums have one fixed order, and which CTA computes an item
+// has no influence on any value: a row's result does not depend on the other rows.  Every CTA (one per SM) takes a stretch of the
+// item list, cut by cost.
 //   warps 0, 3    producers of the even / odd tiles: block-table lookups, TMA loads, exponents
-//   warp 1        issues the MMAs: the scores of tile n + 2 before the output product of tile n
+//   warp 1        issues the MMAs: whichever product can go on, an output product first
 //   warp 2        query tiles, up to two ahead
 //   warps 4-7, 8-11   softmax of even / odd tiles, a thread per cached token
 //   warps 12-15   output: a thread per value dim
 // A second kernel combines a row's splits in ascending order, a third one adds up the weights from the scores that the
 // first wrote (4 bytes per token and column, where mass is wanted).  Every wait is bounded.
+//
+// Bound by the cache's bytes.  64 rows of 512 to 4096 tokens (32 query, 8 key heads of 128, pages of 16): 74 us, of which this kernel 67
+// (50 at the copy rate) and the combine 6.6.  In the middle of a launch a tile of 32 KiB takes an SM 1430 to 1450 cycles, which is the
+// copy rate; the rest is launch, the first tiles (all SMs ask for six at once: the first arrives after 5000 to 13000 cycles), and the
+// last tile's chain of some 4000.  Two rows of 90 K tokens, 4 key heads, pages of 64: 47 us (29 at the copy rate).
+// What brought it there, same case of 64 rows: 121 us with one producer warp and a box each for keys and values; 108 with page numbers and
+// exponents in batches ahead of their use; 90 without integer divisions on the way to the next item (400 to 800 cycles a role); 76 with
+// keys and values of a page in one box (a TMA instruction takes some 70 cycles to issue); 74 with two producers, six tiles in flight and the
+// scores two tiles ahead.
 #include <stddef.h>
 
 #include <atomic>

@@ -1,7 +1,8 @@
 // Rotary positions of queries and keys (include/corun_rope.h): y = rotated x for [T][heads][head_dim].
 //
 // The products are 3 operations a value, so the op is bound by its bytes: each value read and written once.  What would
-// cost more than that is the angle, some 40 instructions a pair: it is computed once and used for many heads.
+// cost more than that is the angle, some 40 instructions a pair: a CTA takes a few tokens, computes their cos and sin once into shared
+// memory and uses them for all of its heads.  4096 tokens of 40 heads of 128 in bf16: 17.4 us (13.0 at the copy rate).
 #include <math.h>
 
 #include <atomic>
