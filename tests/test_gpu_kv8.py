@@ -475,6 +475,42 @@ def test_evict_long_in_place_lengths_and_bad_pages(torch, corun):
         assert np.array_equal(a, b)
 
 
+def test_evict_more_tokens_than_shared_memory_holds(torch, corun):
+    ctx = [50001, 300]
+    s = Setup(torch, corun, ctx, 1, 64, 64, seed=12)
+    m = (s.rng.random((2, 1, s.max_blocks * 64)) ** 2).astype(np.float32)
+    m[:, :, ::5] = 0.5
+    mass = torch.tensor(m).cuda()
+    kept, new_ctx = s.cache.evict(_i32(torch, ctx), s.t_table, mass, _i32(torch, [9000, 9000]), 9000, sinks=1, recent=7)
+    assert new_ctx.tolist() == [9000, 300] and bool((kept[1] == -1).all())
+    src = s.want.evict(s.table[0], 50001, m[0], 9000, 1, 7)
+    assert np.array_equal(kept[0].cpu().numpy(), src) and np.array_equal(mass.cpu().numpy(), m)
+    got = ko.Cache(*s.state())
+    for a, b in zip(got.values(s.table[0], 9000), s.want.values(s.table[0], 9000)):
+        assert np.array_equal(a, b)
+
+
+def test_many_rows_are_what_few_rows_are(torch, corun):
+    """300 rows in one call, empty ones among them: the bytes of six calls of 50."""
+    rng = np.random.default_rng(3)
+    ctx = [int(c) if c > 20 else 0 for c in rng.integers(0, 400, 300)]
+    s = Setup(torch, corun, [max(c, 1) for c in ctx], 2, 64, 16, seed=13)
+    other = corun.Kv8Cache(s.cache.pages, 2, 64, 16, pool=s.cache.pool.clone(), exps=s.cache.exps.clone())
+    mk = lambda h: torch.tensor(rng.standard_normal((300, h, 64))).to(torch.float16).cuda()
+    q, k, v, pos = mk(6), mk(2), mk(2), _i32(torch, rng.integers(0, 9999, 300))
+    rope, t_ctx = corun.Rope(64), _i32(torch, ctx)
+    q_all = s.cache.append(k, v, t_ctx, s.t_table, positions=pos, rope=rope, q=q, q_out=torch.zeros_like(q))
+    out = corun.Kv8Attention(300, 6, 2, 64, s.max_blocks, 16).run(q_all, s.cache, t_ctx, s.t_table, 0.02)
+    att = corun.Kv8Attention(50, 6, 2, 64, s.max_blocks, 16)
+    for i in range(0, 300, 50):
+        part = slice(i, i + 50)
+        qp = other.append(k[part], v[part], t_ctx[part], s.t_table[part], positions=pos[part], rope=rope, q=q[part], q_out=torch.zeros_like(q[part]))
+        o = att.run(qp, other, t_ctx[part], s.t_table[part], 0.02)
+        att.sync()
+        assert torch.equal(q_all[part], qp) and torch.equal(out[part], o)
+    assert torch.equal(s.cache.pool.view(torch.uint8), other.pool.view(torch.uint8)) and torch.equal(s.cache.exps, other.exps)
+
+
 # ---------------------------------------------------------------- together
 
 def test_decode_with_eviction(torch, corun):
