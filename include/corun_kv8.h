@@ -43,7 +43,8 @@ typedef struct {
   const int32_t *cu;    /* int32 [B + 1]: row b's tokens of this call are cu[b] .. cu[b + 1] - 1, its last ones in
                            the cache; NULL: one token per row, token b being row b's             */
   int32_t B;            /* 1..65535                                                             */
-  int32_t T;            /* tokens there is room for (cu[B] <= T; NULL cu: B)                    */
+  int32_t T;            /* tokens there is room for (cu[B] <= T; NULL cu: B); 0: a call that reads and writes nothing,
+                           whose data pointers may be NULL                                      */
 } corun_kv8_rows;
 
 /*
@@ -72,8 +73,9 @@ int corun_kv8_append(const corun_kv8_cache *cache, const corun_kv8_rows *rows, c
  * A NaN among the values of a token reaches every query that sees the token, and may reach other queries of the same row and call.
  * n_q a multiple of n_kv, n_q / n_kv <= 32, B <= 512, scale > 0, T / (128 / (n_q / n_kv)) + B at most some 65000 (EINVAL beyond).  Queries and softmax weights enter the tensor cores as
  * sums of e4m3 values that hold 11 or more bits of them; scores, weights' sums and outputs are held in 32 bits.
- * Errors: EINVAL, ECUDA.  A bounded device-side wait that expires is recorded in ws: corun_kv8_sync waits for the
- * stream and returns ETIMEOUT in that case.
+ * Errors: EINVAL, ECUDA.  A bounded device-side wait that expires is recorded in the first 1024 bytes of ws: corun_kv8_sync waits for
+ * the stream and returns ETIMEOUT in that case.  With T 0 corun_kv8_attend_bytes is 0 and ws may be NULL; where it has 1024 bytes or more,
+ * those are cleared.  corun_kv8_sync is for a ws that has them.
  */
 int64_t corun_kv8_attend_bytes(int32_t B, int32_t T, int32_t max_new, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t block,
                                int32_t max_blocks, int32_t with_mass);

@@ -914,7 +914,7 @@ class Kv8Attention:
         # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
         ws = T.empty(max(n_ws, 1), dtype=T.uint8, device=dev)
         _launch(lib().corun_kv8_attend, "corun_kv8_attend", dev, cache._c, r, self.max_new, qh, oh, code, n_q, scale, window, m, ws.data_ptr(), n_ws)
-        self.ws = ws
+        self.ws = ws if n else None                             # (a call without tokens has no status)
         return out
 
     def sync(self):

@@ -399,13 +399,14 @@ using namespace corun;
 extern "C" int corun_kv8_append(const corun_kv8_cache *cache, const corun_kv8_rows *rows, const corun_heads *k, const corun_heads *v,
                                 int32_t dtype, const corun_rope *rope, const int32_t *positions, const corun_heads *q,
                                 const corun_heads *q_out, int32_t n_q, float *mass, void *cuda_stream) {
-  if (!kv8_cache_ok(cache) || !kv8_rows_ok(rows, cache) || !k || !v || !k->p || !v->p || dtype < CORUN_F32 || dtype > CORUN_F16) return CORUN_EINVAL;
+  if (!kv8_cache_ok(cache) || !kv8_rows_ok(rows, cache) || !k || !v || dtype < CORUN_F32 || dtype > CORUN_F16) return CORUN_EINVAL;
+  if (q && (!q_out || n_q < 1 || n_q > 65535)) return CORUN_EINVAL;
+  if (rope && rope->t.rot > cache->head_dim) return CORUN_EINVAL;
+  if (rows->T == 0) return CORUN_OK;               // (tensors of no tokens may have no address)
   const uintptr_t sz = (uintptr_t)dtype_size(dtype);
-  if (!aligned_to(k->p, sz) || !aligned_to(v->p, sz)) return CORUN_EINVAL;
-  if (q && (!q->p || !q_out || !q_out->p || n_q < 1 || n_q > 65535 || !aligned_to(q->p, sz) || !aligned_to(q_out->p, sz))) return CORUN_EINVAL;
+  if (!k->p || !v->p || !aligned_to(k->p, sz) || !aligned_to(v->p, sz) || (rope && !positions)) return CORUN_EINVAL;
+  if (q && (!q->p || !q_out->p || !aligned_to(q->p, sz) || !aligned_to(q_out->p, sz))) return CORUN_EINVAL;
   if (q && q->p == q_out->p && (q->token_stride != q_out->token_stride || q->head_stride != q_out->head_stride)) return CORUN_EINVAL;
-  if (rope && (!positions || rope->t.rot > cache->head_dim)) return CORUN_EINVAL;
-  if (rows->T == 0) return CORUN_OK;
   int dev = 0, sms = 0;
   cudaError_t ce = device_sms(&dev, &sms);
   if (ce != cudaSuccess || sms < 1) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }

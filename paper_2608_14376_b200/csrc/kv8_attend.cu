@@ -929,13 +929,17 @@ int64_t corun_kv8_attend_bytes(int32_t B, int32_t T, int32_t max_new, int32_t n_
 int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, int32_t max_new, const corun_heads *q,
                      const corun_heads *out, int32_t dtype, int32_t n_q, float scale, int32_t window, float *mass, void *ws,
                      int64_t ws_bytes, void *cuda_stream) {
-  if (!kv8_cache_ok(cache) || !kv8_rows_ok(rows, cache) || !q || !out || !q->p || !out->p || (dtype != CORUN_BF16 && dtype != CORUN_F16) ||
+  if (!kv8_cache_ok(cache) || !kv8_rows_ok(rows, cache) || !q || !out || (dtype != CORUN_BF16 && dtype != CORUN_F16) ||
       rows->B > AT_MAXB || max_new < 1 || (!rows->cu && max_new != 1) || n_q < 1 || n_q % cache->n_kv || n_q / cache->n_kv > AT_MAXC || !(scale > 0.f) || isinf(scale) ||
-      window < 0 || (mass && (int64_t)max_new * (n_q / cache->n_kv) > AT_MAXC) || !heads_on_16(*q, dtype) || !heads_on_16(*out, dtype) || !ws ||
-      kv8_chunk_tiles(rows->T, rows->B, n_q / cache->n_kv) > 65535 ||
-      !aligned_to(ws, 256))
+      window < 0 || (mass && (int64_t)max_new * (n_q / cache->n_kv) > AT_MAXC) || kv8_chunk_tiles(rows->T, rows->B, n_q / cache->n_kv) > 65535)
     return CORUN_EINVAL;
-  if (rows->T == 0) return CORUN_OK;
+  if (rows->T == 0) {                               // (tensors of no tokens may have no address)
+    if (!ws || ws_bytes < AT_STATUS * (int)sizeof(int)) return CORUN_OK;
+    const cudaError_t ce = cudaMemsetAsync(ws, 0, AT_STATUS * sizeof(int), (cudaStream_t)cuda_stream);
+    if (ce != cudaSuccess) { g_last_cuda_error = (int)ce; return CORUN_ECUDA; }
+    return CORUN_OK;
+  }
+  if (!q->p || !out->p || !heads_on_16(*q, dtype) || !heads_on_16(*out, dtype) || !ws || !aligned_to(ws, 256)) return CORUN_EINVAL;
   const AttendSpace s = attend_space(rows->B, max_new, n_q, cache->n_kv, cache->head_dim, cache->block, rows->max_blocks, mass != nullptr);
   if (ws_bytes < s.bytes) return CORUN_EINVAL;
   int dev = 0, sms = 0;

@@ -1,0 +1,39 @@
+"""Calls of the 8-bit cache's operators that their documentation allows: none of them goes through the shapes of
+``test_gpu_kv8.py``.  Tolerances are that file's."""
+import numpy as np
+import pytest
+
+from oracle import kv8_oracle as ko
+from tests.test_gpu_kv8 import Setup, _check_attend, _check_values, _eps, _i32, _np, corun, torch  # noqa: F401 (fixtures)
+
+pytestmark = pytest.mark.gpu
+
+
+def _decode_call(torch, s, n_q, seed=0, dtype="bfloat16"):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(s.table.shape[0], n_q, s.hd, generator=g) * 0.1).to(getattr(torch, dtype)).cuda()
+
+
+# ---------------------------------------------------------------- calls without tokens
+
+def test_calls_without_tokens(torch, corun):
+    """A step in which no row brings a token: nothing is read or written, nothing raised."""
+    s = Setup(torch, corun, [40, 7], 2, 64, 16, seed=1)
+    before = s.state()
+    ctx, cu = _i32(torch, [40, 7]), _i32(torch, [0, 0, 0])
+    empty = lambda heads: torch.empty(0, heads, 64, dtype=torch.bfloat16, device="cuda")
+    pos = torch.empty(0, dtype=torch.int32, device="cuda")
+    mass = torch.full((2, 2, s.max_blocks * 16), 3.0, device="cuda")
+    assert s.cache.append(empty(2), empty(2), ctx, s.t_table, cu=cu, mass=mass) is None
+    q = s.cache.append(empty(2), empty(2), ctx, s.t_table, cu=cu, positions=pos, rope=corun.Rope(64), q=empty(8), mass=mass)
+    assert q.shape == (0, 8, 64)
+    att = corun.Kv8Attention(2, 8, 2, 64, s.max_blocks, 16, tokens=8, max_new=4)
+    assert att.run(q, s.cache, ctx, s.t_table, 0.1, cu=cu, mass=mass).shape == (0, 8, 64)
+    att.sync()
+    # behind a call with tokens, too
+    x = _decode_call(torch, s, 8)
+    att.run(x, s.cache, ctx, s.t_table, 0.1, cu=_i32(torch, [0, 1, 2]))
+    att.run(q, s.cache, ctx, s.t_table, 0.1, cu=cu, mass=mass)
+    att.sync()
+    after = s.state()
+    assert np.array_equal(before[0], after[0]) and np.array_equal(before[1], after[1]) and bool((mass == 3).all())

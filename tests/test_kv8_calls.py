@@ -1,0 +1,27 @@
+"""Calls of the 8-bit cache's operators that come back before any CUDA call: calls without tokens, objects that were closed, workspaces."""
+import ctypes as C
+
+import pytest
+import torch
+
+from tests.test_kv8_oracle import BASE, _parts, lib  # noqa: F401 (lib: a fixture)
+
+
+def test_no_tokens_need_no_data(lib):
+    """A call without tokens reads no tensor: an empty one has no address."""
+    corun, cache, rows, x = _parts()
+    rows.T, rows.cu = 0, BASE
+    c, r, none = C.byref(cache), C.byref(rows), C.byref(corun.Heads(None, 1024, 128))
+    rope = corun.Rope(128)
+    assert lib.corun_kv8_append(c, r, none, none, 1, None, None, None, None, 0, None, None) == corun.OK
+    assert lib.corun_kv8_append(c, r, none, none, 1, rope._h, None, none, none, 32, None, None) == corun.OK
+    assert lib.corun_kv8_attend(c, r, 4, none, none, 1, 32, 0.1, 0, None, None, 0, None) == corun.OK
+    # the rest is checked all the same
+    assert lib.corun_kv8_append(c, r, none, none, 3, None, None, None, None, 0, None, None) == corun.EINVAL
+    assert lib.corun_kv8_append(c, r, none, none, 1, None, None, none, none, 0, None, None) == corun.EINVAL
+    assert lib.corun_kv8_append(c, r, None, none, 1, None, None, None, None, 0, None, None) == corun.EINVAL
+    assert lib.corun_kv8_attend(c, r, 0, none, none, 1, 32, 0.1, 0, None, None, 0, None) == corun.EINVAL
+    assert lib.corun_kv8_attend(c, r, 4, none, none, 1, 12, 0.1, 0, None, None, 0, None) == corun.EINVAL
+    assert lib.corun_kv8_attend(c, r, 4, none, None, 1, 32, 0.1, 0, None, None, 0, None) == corun.EINVAL
+    rows.cu = None                                              # one token each: not none
+    assert lib.corun_kv8_append(c, r, none, none, 1, None, None, None, None, 0, None, None) == corun.EINVAL
