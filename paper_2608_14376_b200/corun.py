@@ -907,13 +907,14 @@ class Kv8Attention:
         oh = _heads(out, (n, n_q, hd), dt, dev, "out")
         r = cache._rows(ctx, block_table, cu, n)
         m = cache._mass(mass, block_table)
-        key = (n, m is not None)
+        max_new = self.max_new if cu is not None else 1
+        key = (n, max_new, m is not None)
         n_ws = self._bytes.get(key)
         if n_ws is None:
-            n_ws = self._bytes[key] = lib().corun_kv8_attend_bytes(rows, n, self.max_new, n_q, n_kv, hd, block, max_blocks, int(key[1]))
+            n_ws = self._bytes[key] = lib().corun_kv8_attend_bytes(rows, n, max_new, n_q, n_kv, hd, block, max_blocks, int(key[2]))
         # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
         ws = T.empty(max(n_ws, 1), dtype=T.uint8, device=dev)
-        _launch(lib().corun_kv8_attend, "corun_kv8_attend", dev, cache._c, r, self.max_new, qh, oh, code, n_q, scale, window, m, ws.data_ptr(), n_ws)
+        _launch(lib().corun_kv8_attend, "corun_kv8_attend", dev, cache._c, r, max_new, qh, oh, code, n_q, scale, window, m, ws.data_ptr(), n_ws)
         self.ws = ws if n else None                             # (a call without tokens has no status)
         return out
 

@@ -37,3 +37,22 @@ def test_calls_without_tokens(torch, corun):
     att.sync()
     after = s.state()
     assert np.array_equal(before[0], after[0]) and np.array_equal(before[1], after[1]) and bool((mass == 3).all())
+
+
+# ---------------------------------------------------------------- calls of the binding
+
+def test_one_token_each_where_more_are_allowed(torch, corun):
+    """An object made for several tokens a row serves a call without cu (one token each), with the same bytes."""
+    s = Setup(torch, corun, [300, 0, 17], 2, 128, 16, seed=2)
+    q, ctx = _decode_call(torch, s, 8), _i32(torch, [300, 0, 17])
+    want = corun.Kv8Attention(3, 8, 2, 128, s.max_blocks).run(q, s.cache, ctx, s.t_table, 0.1)
+    for max_new in (4, 100):
+        att = corun.Kv8Attention(3, 8, 2, 128, s.max_blocks, tokens=100, max_new=max_new)
+        assert torch.equal(att.run(q, s.cache, ctx, s.t_table, 0.1), want)
+        att.sync()
+        # with weights: a row's own columns count, not those of the largest call
+        mass = torch.zeros(3, 2, s.max_blocks * 16, device="cuda")
+        assert torch.equal(att.run(q, s.cache, ctx, s.t_table, 0.1, mass=mass), want)
+        att.sync()
+        got = _np(mass.sum(-1))                                 # 4 heads of a key head; each weight within 2^-21 or so of its own
+        assert np.all(np.abs(got - np.array([[4.0], [0.0], [4.0]])) <= 4 * (2.0 ** -16 + 300 * 2.0 ** -24))
