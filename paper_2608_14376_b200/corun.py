@@ -889,7 +889,7 @@ class Kv8Attention:
     def __init__(self, rows: int, n_q: int, n_kv: int, head_dim: int, max_blocks: int, block: int = 16, tokens: int = 0, max_new: int = 1):
         self.shape = (rows, n_q, n_kv, head_dim, max_blocks, block)
         self.tokens, self.max_new = tokens or rows, max_new
-        self._bytes, self.ws = {}, None
+        self._bytes, self._last = {}, None                       # workspace sizes; the last call's workspace and stream
 
     def run(self, q, cache: "Kv8Cache", ctx, block_table, scale: float, cu=None, window: int = 0, mass=None, out=None):
         """q [tokens, n_q, head_dim] (bf16 or fp16) -> out (default: a new tensor, zeros where no row writes): the rows' last cached
@@ -915,13 +915,20 @@ class Kv8Attention:
         # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
         ws = T.empty(max(n_ws, 1), dtype=T.uint8, device=dev)
         _launch(lib().corun_kv8_attend, "corun_kv8_attend", dev, cache._c, r, max_new, qh, oh, code, n_q, scale, window, m, ws.data_ptr(), n_ws)
-        self.ws = ws if n else None                             # (a call without tokens has no status)
+        # (a call without tokens has no status)
+        self._last = (ws, _stream_of(dev.index)) if n else None
         return out
 
     def sync(self):
-        """Waits for the stream; raises if a bounded device-side wait of the last call expired."""
-        if self.ws is not None:
-            _launch(lib().corun_kv8_sync, "corun_kv8_sync", self.ws.device, self.ws.data_ptr())
+        """Waits for the last call's stream and for the current one (a captured call may have been replayed on it); raises if a
+        bounded device-side wait of the last call expired.  Threads that look at their own calls take an object each."""
+        last = self._last
+        if last is not None:
+            ws, stream = last
+            if stream != _stream_of(ws.device.index):
+                T = _torch()
+                (T.cuda.ExternalStream(stream, device=ws.device) if stream else T.cuda.default_stream(ws.device)).synchronize()
+            _launch(lib().corun_kv8_sync, "corun_kv8_sync", ws.device, ws.data_ptr())
 
 
 MICROBENCH_KINDS = ("rmsnorm", "softmax", "column_sum")

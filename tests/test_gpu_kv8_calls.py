@@ -56,3 +56,26 @@ def test_one_token_each_where_more_are_allowed(torch, corun):
         att.sync()
         got = _np(mass.sum(-1))                                 # 4 heads of a key head; each weight within 2^-21 or so of its own
         assert np.all(np.abs(got - np.array([[4.0], [0.0], [4.0]])) <= 4 * (2.0 ** -16 + 300 * 2.0 ** -24))
+
+
+def test_sync_waits_for_the_call(torch, corun):
+    """``sync`` waits for the last call whatever stream is current, and behind a replay for the current stream."""
+    s = Setup(torch, corun, [300, 17], 2, 64, 16, seed=3)
+    q, ctx = _decode_call(torch, s, 8), _i32(torch, [300, 17])
+    att = corun.Kv8Attention(2, 8, 2, 64, s.max_blocks)
+    want = att.run(q, s.cache, ctx, s.t_table, 0.1)
+    att.sync()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)                          # some 100 ms
+        out = att.run(q, s.cache, ctx, s.t_table, 0.1)
+    att.sync()
+    assert side.query() and torch.equal(out, want)
+    g, out = torch.cuda.CUDAGraph(), torch.zeros_like(want)
+    with torch.cuda.graph(g):
+        torch.cuda._sleep(200_000_000)
+        att.run(q, s.cache, ctx, s.t_table, 0.1, out=out)
+    g.replay()
+    att.sync()
+    assert torch.cuda.current_stream().query() and torch.equal(out, want)
