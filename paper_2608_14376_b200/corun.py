@@ -839,7 +839,7 @@ class Kv8Cache:
     def append(self, k, v, ctx, block_table, cu=None, positions=None, rope: "Rope" = None, q=None, q_out=None, mass=None):
         """Appends k, v [tokens, n_kv, head_dim]: ``ctx`` int32 [rows] counts every row's cached tokens with the new ones, ``cu``
         int32 [rows + 1] says which tokens are whose (None: one each).  ``rope`` rotates keys and q [tokens, n_q, head_dim] at
-        ``positions`` int32 [tokens].  Returns the queries (``q_out``, or a new tensor), None without q; ``mass`` float32
+        ``positions`` int32 [tokens].  Returns the queries (``q_out``, or a new tensor, zeros for tokens of no row), None without q; ``mass`` float32
         [rows, n_kv, blocks * block]: the new tokens' accumulated weights become 0.  Asynchronous on torch's current stream."""
         T, code, dt, dev = _torch(), _dtype_code(k, "k"), k.dtype, self.device
         n, n_kv, hd = k.shape[0], self.n_kv, self.head_dim
@@ -852,7 +852,7 @@ class Kv8Cache:
             n_q = q.shape[1]
             qh = _heads(q, (n, n_q, hd), dt, dev, "q")
             if q_out is None:
-                q_out = T.empty((n, n_q, hd), dtype=dt, device=dev)
+                q_out = T.zeros((n, n_q, hd), dtype=dt, device=dev)
             oh = _heads(q_out, (n, n_q, hd), dt, dev, "q_out")
         if rope is not None and positions is None:
             raise ValueError("rope needs positions")

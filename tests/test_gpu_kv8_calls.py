@@ -79,3 +79,16 @@ def test_sync_waits_for_the_call(torch, corun):
     g.replay()
     att.sync()
     assert torch.cuda.current_stream().query() and torch.equal(out, want)
+
+
+def test_append_without_out_leaves_zeros(torch, corun):
+    """The queries that ``append`` returns: zeros for tokens of no row, whatever the memory held before."""
+    s = Setup(torch, corun, [40, 0, 7], 2, 128, 16, seed=4)
+    x = _decode_call(torch, s, 12)
+    q, k, v = x[:, :8], x[:, 8:10], x[:, 10:]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    used = torch.full((3, 8, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    del used                                                    # its memory is the next call's
+    out = s.cache.append(k, v, _i32(torch, [40, 0, 7]), s.t_table, q=q)
+    assert torch.equal(out[::2], q[::2]) and bool((out[1] == 0).all())
