@@ -781,11 +781,17 @@ class Rope:
         _check(lib().corun_rope_create(C.byref(c), C.byref(h)), "corun_rope_create")
         self._h, self.rot_dim = h, rot_dim
 
+    def _handle(self):
+        if self._h is None:                                     # (to append, no handle means no rotation)
+            raise ValueError("the Rope is closed")
+        return self._h
+
     def apply(self, x, positions, out=None):
         """x [tokens, heads, dims] (fp32, bf16 or fp16, any strides of tokens and heads), positions int32 [tokens] -> rotated
         values in ``out`` (default: a new tensor; may be x).  Asynchronous on torch's current stream."""
         if x.dim() != 3:
             raise ValueError(f"x: [tokens, heads, dims] is needed, not {tuple(x.shape)}")
+        h = self._handle()
         T, code, dev = _torch(), _dtype_code(x, "x"), x.device
         n, heads, dims = shape = x.shape
         xh = _heads(x, shape, x.dtype, dev, "x")
@@ -793,7 +799,7 @@ class Rope:
         yh = _heads(y, shape, x.dtype, dev, "out")
         pos = _plain(positions, (n,), T.int32, dev, "positions")
         if n and heads and dims:
-            _launch(lib().corun_rope_apply, "corun_rope_apply", dev, self._h, xh, yh, code, pos, n, heads, dims)
+            _launch(lib().corun_rope_apply, "corun_rope_apply", dev, h, xh, yh, code, pos, n, heads, dims)
         return y
 
     def close(self):
@@ -854,10 +860,11 @@ class Kv8Cache:
             if q_out is None:
                 q_out = T.zeros((n, n_q, hd), dtype=dt, device=dev)
             oh = _heads(q_out, (n, n_q, hd), dt, dev, "q_out")
+        rh = rope._handle() if rope is not None else None
         if rope is not None and positions is None:
             raise ValueError("rope needs positions")
         pos = _plain(positions, (n,), T.int32, dev, "positions") if positions is not None else None
-        _launch(lib().corun_kv8_append, "corun_kv8_append", dev, self._c, rows, kh, vh, code, rope._h if rope is not None else None, pos, qh, oh, n_q,
+        _launch(lib().corun_kv8_append, "corun_kv8_append", dev, self._c, rows, kh, vh, code, rh, pos, qh, oh, n_q,
                 self._mass(mass, block_table))
         return q_out if q is not None else None
 

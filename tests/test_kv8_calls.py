@@ -25,3 +25,18 @@ def test_no_tokens_need_no_data(lib):
     assert lib.corun_kv8_attend(c, r, 4, none, None, 1, 32, 0.1, 0, None, None, 0, None) == corun.EINVAL
     rows.cu = None                                              # one token each: not none
     assert lib.corun_kv8_append(c, r, none, none, 1, None, None, None, None, 0, None, None) == corun.EINVAL
+
+
+def test_a_closed_rope_is_refused(lib):
+    """append with a closed ``Rope`` does not go on without rotating."""
+    from paper_2608_14376_b200 import corun
+
+    rope = corun.Rope(64)
+    rope.close()
+    rope.close()
+    cache = corun.Kv8Cache(4, 2, 64, device="cpu")
+    k, one = torch.zeros(1, 2, 64), torch.ones(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="closed"):
+        cache.append(k, k, one, torch.zeros(1, 4, dtype=torch.int32), positions=one, rope=rope)
+    with pytest.raises(ValueError, match="closed"):
+        rope.apply(k, one)
