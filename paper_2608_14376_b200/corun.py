@@ -876,6 +876,8 @@ class Kv8Cache:
         rows = self._rows(ctx, block_table, None, B)
         if mass is None:
             raise ValueError("mass is needed")
+        if sinks >> 31 not in (0, -1) or recent >> 31 not in (0, -1):
+            raise ValueError(f"sinks {sinks}, recent {recent}: 0 or more is needed, max_keep together at most")
         m = self._mass(mass, block_table)
         kp = _plain(keep, (B,), T.int32, dev, "keep")
         if new_ctx is None:
@@ -915,6 +917,8 @@ class Kv8Attention:
         r = cache._rows(ctx, block_table, cu, n)
         m = cache._mass(mass, block_table)
         max_new = self.max_new if cu is not None else 1
+        if window >> 31:                                        # beyond 32 bits: wider than any cache, as all of 2^30 and above, or refused
+            window = 0 if window > 0 else -1
         key = (n, max_new, m is not None)
         n_ws = self._bytes.get(key)
         if n_ws is None:

@@ -1,5 +1,7 @@
 """Calls of the 8-bit cache's operators that their documentation allows: none of them goes through the shapes of
 ``test_gpu_kv8.py``.  Tolerances are that file's."""
+import sys
+
 import numpy as np
 import pytest
 
@@ -92,3 +94,15 @@ def test_append_without_out_leaves_zeros(torch, corun):
     del used                                                    # its memory is the next call's
     out = s.cache.append(k, v, _i32(torch, [40, 0, 7]), s.t_table, q=q)
     assert torch.equal(out[::2], q[::2]) and bool((out[1] == 0).all())
+
+
+@pytest.mark.parametrize("window", [2 ** 30, 2 ** 31, 2 ** 32, 2 ** 32 + 5, sys.maxsize])
+def test_windows_beyond_the_cache(torch, corun, window):
+    """A window wider than any cache is no window."""
+    s = Setup(torch, corun, [300, 17], 2, 64, 16, seed=5)
+    q, ctx = _decode_call(torch, s, 8), _i32(torch, [300, 17])
+    att = corun.Kv8Attention(2, 8, 2, 64, s.max_blocks)
+    want = att.run(q, s.cache, ctx, s.t_table, 0.1)
+    assert torch.equal(att.run(q, s.cache, ctx, s.t_table, 0.1, window=window), want)
+    with pytest.raises(corun.CorunError):
+        att.run(q, s.cache, ctx, s.t_table, 0.1, window=-window)

@@ -40,3 +40,14 @@ def test_a_closed_rope_is_refused(lib):
         cache.append(k, k, one, torch.zeros(1, 4, dtype=torch.int32), positions=one, rope=rope)
     with pytest.raises(ValueError, match="closed"):
         rope.apply(k, one)
+
+
+@pytest.mark.parametrize("sinks,recent", [(2 ** 32, 4), (4, 2 ** 32), (2 ** 32 + 4, 2 ** 32 + 4), (4, -2 ** 32 + 4)])
+def test_evict_refuses_counts_beyond_32_bits(sinks, recent):
+    """What the library would get in 32 bits is another number."""
+    from paper_2608_14376_b200 import corun
+
+    cache = corun.Kv8Cache(4, 2, 64, device="cpu")
+    one, table = torch.ones(1, dtype=torch.int32), torch.zeros(1, 4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="sinks"):
+        cache.evict(one, table, torch.zeros(1, 2, 64), one, 32, sinks=sinks, recent=recent)
