@@ -603,7 +603,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
           const float4 f = *reinterpret_cast<const float4 *>(xm[lane]);
           m_tile = fmaxf(fmaxf(fmaxf(f.x, f.y), fmaxf(f.z, f.w)), AT_LOW);
           const float m_new = fmaxf(m_run, m_tile);
-          ab[lane] = make_float4(ex2(m_run - m_new), ex2(m_tile - m_new), m_tile - 8.f, 0.f);
+          // (beyond 2^27 in magnitude the subtraction may take 16 away, and 2^16 would be beyond fp16: weights up to 1 then)
+          const float low = m_tile - 8.f;
+          ab[lane] = make_float4(ex2(m_run - m_new), ex2(m_tile - m_new), m_tile - low > 9.f ? m_tile : low, 0.f);
           m_run = m_new;
         }
         // the frames of the group's tile before must have been read; its output product, and so its weights, then too

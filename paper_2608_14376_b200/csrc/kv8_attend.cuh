@@ -10,7 +10,7 @@ constexpr int AT_T = 128;           // cached tokens per tile
 constexpr int AT_MAXC = 32;         // columns of a row that is split over its cached tokens
 constexpr int AT_MAXB = 512;        // rows per call: a thread plans one
 constexpr int AT_STATUS = 256;      // status words at the start of the workspace
-constexpr float AT_LOW = -1e30f;    // a maximum over nothing
+constexpr float AT_LOW = -3.4028235e38f;   // a maximum over nothing: no finite score is below it
 
 struct AttendArgs {
   const int8_t *exps;

@@ -106,3 +106,38 @@ def test_windows_beyond_the_cache(torch, corun, window):
     assert torch.equal(att.run(q, s.cache, ctx, s.t_table, 0.1, window=window), want)
     with pytest.raises(corun.CorunError):
         att.run(q, s.cache, ctx, s.t_table, 0.1, window=-window)
+
+
+# ---------------------------------------------------------------- numbers
+
+def _one_token_takes_all(torch, corun, G, hd, n, scale, sign):
+    """Only the first dim of queries and keys is not 0, so a score is one product; the largest one is apart from the others by at least
+    1.25 * scale, and its token takes all the weight."""
+    c, n_kv = 300, 2
+    s = Setup(torch, corun, [c], n_kv, hd, 16, seed=7)
+    codes, exps = s.codes.copy(), s.exps.copy()
+    codes[:, 0], exps[:, 0] = 0, 0
+    far = int(s.rng.integers(0, c - n + 1))                     # (seen by every query of the call)
+    for j in range(c):                                          # 1 or 256 for one token, 2.25 to 240 for the others
+        codes[s.table[0, j // 16], 0, :, j % 16, 0] = (0x38 if sign < 0 else 0x78) if j == far else 0x41 + int(s.rng.integers(0, 0x37))
+    s.cache.pool.copy_(torch.tensor(codes).cuda().view(torch.float8_e4m3fn))
+    s.cache.exps.copy_(torch.tensor(exps))
+    s.want = ko.Cache(codes, exps)
+    q = torch.zeros(n, G * n_kv, hd, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = sign
+    att = corun.Kv8Attention(1, G * n_kv, n_kv, hd, s.max_blocks, tokens=n, max_new=n)
+    out = att.run(q, s.cache, _i32(torch, [c]), s.t_table, scale, cu=_i32(torch, [0, n]))
+    att.sync()
+    v = np.repeat(s.want.values(s.table[0], c)[1][far], G, 0)
+    # one weight of 1: what is left is its rounding with the value's (11 bits, the sum of weights alike) and the output's
+    assert np.all(np.abs(_np(out) - v) <= (_eps(torch, torch.bfloat16) + 2 * 2.0 ** -11) * np.abs(v))
+
+
+HUGE = [1e6, 1e8, 3e8, 1e9, 1e20, 1e32]
+
+
+@pytest.mark.parametrize("G,hd,n", [(4, 128, 1), (8, 64, 1), (16, 128, 1), (2, 128, 3)])
+@pytest.mark.parametrize("scale", HUGE)
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_attend_huge_scores(torch, corun, G, hd, n, scale, sign):
+    _one_token_takes_all(torch, corun, G, hd, n, scale, sign)
