@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
   __shared__ float max_s[4][128], sum_s[4][128];    // a block's frame and sum per row, four blocks in turn
   __shared__ float q_mul[128];                      // 2^e of a query row times scale log2(e)
   __shared__ int8_t exps[CH_EXPS][2][8];
+  __shared__ float k_top[CH_EXPS];                  // the largest of the keys' scales
   __shared__ int row_c[AT_MAXB], row_tiles[AT_MAXB], s_row, s_qt, s_c, s_first, s_n;
   __shared__ uint32_t tmem_base_s;
   __shared__ int abort_flag;
@@ -127,10 +128,11 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
   // producers: lane l fetches page l of a block; its page number is read two blocks ahead of its use, its exponents one
   const bool keys = warp == 16;
   const int *table = a.block_table + (size_t)s_row * a.max_blocks;
-  int page0 = -1, page1 = -1, ek = 0, ev = 0;
+  int page0 = -1, page1 = -1, ek = KV8_E_MIN, ev = 0;
   auto page_at = [&](int j) { return j < n_blocks && lane < pages_of(j) ? load_now(table + ((b0 + j) * (AT_T >> shift) + lane)) : -1; };
   auto exps_at = [&](int page) {
-    ek = ev = 0;
+    ek = KV8_E_MIN;                                 // (of a page that is not there: its keys are zeros, or nobody sees them)
+    ev = 0;
     if (keys && page >= 0 && (long long)page < a.pages) {
       const long long at = (long long)page * 2 * a.n_kv + g;
       ek = load_now(a.exps + at);
@@ -152,6 +154,8 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
       // (the keys of block j - CH_KR, whose slot this is, were turned behind the output of block j - 5: what read the exponents of block
       // j - CH_EXPS has ended)
       if (lane < 8) { exps[j % CH_EXPS][0][lane] = (int8_t)ek_now; exps[j % CH_EXPS][1][lane] = (int8_t)ev_now; }
+      const int top = __reduce_max_sync(0xffffffffu, ek_now);
+      if (lane == 0) k_top[j % CH_EXPS] = pow2f(top);
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&e_full[j % CH_EXPS]));
       exps_at(page0);
@@ -252,13 +256,17 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     const int sb = warp >> 2;
     const uint32_t st = t_lane + (uint32_t)(sb * 128), pt = t_lane + L::P_COL + (uint32_t)(sb * 64);
     for (int j = sb; j < n_blocks; j += 2) {
-      if (!wait_all(e_full[j % CH_EXPS], (uint32_t)(j / CH_EXPS)) || !wait_all(s_full[sb], (uint32_t)(j >> 1))) break;
-      tc_fence_after();
+      if (!wait_all(e_full[j % CH_EXPS], (uint32_t)(j / CH_EXPS))) break;
       const int8_t *ex = exps[j % CH_EXPS][0];
+      // x f + (e_v - M) is rounded once where M was rounded before: they differ by up to |M| 2^-24, which is nothing while |M| stays below 2^20,
+      // but takes weights beyond fp16 from 2^28 on.  |x| is below 2^25: where a score might pass 2^20, the exponents are formed as M was.
+      const bool far = k_top[j % CH_EXPS] * qm > 0.03125f;
+      if (!wait_all(s_full[sb], (uint32_t)(j >> 1))) break;
+      tc_fence_after();
       const int lim = pos - (b0 + j) * AT_T, low = a.window ? lim - a.window : -1;   // tokens low + 1 .. lim of the block are visible
       float bm = -CUDART_INF_F, l = 0.f;
-      auto block = [&](auto masked) {
-        constexpr bool M = decltype(masked)::value;
+      auto block = [&](auto masked, auto may_be_far) {
+        constexpr bool M = decltype(masked)::value, FAR = decltype(may_be_far)::value;
         uint32_t v[2][16];
         tmem_ld16(st, v[0]);
         auto largest = [&](const uint32_t (&x)[16], int c) {        // chunk c: tokens 16 c .. 16 c + 15, all of one page
@@ -284,13 +292,17 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
         if (j > 1 && !wait_all(p_free[sb], (uint32_t)((j >> 1) - 1))) return;
         auto weights = [&](const uint32_t (&x)[16], int c) {
           const int p = (16 * c) >> shift, ev = ex[8 + p];
-          const float f = pow2f(ex[p]) * qm, off = (float)ev - ref;
+          const float f = pow2f(ex[p]) * qm, off = FAR ? (float)ev : (float)ev - ref;
+          auto weight = [&](uint32_t s) {
+            const float y = fmaf(__uint_as_float(s), f, off);
+            return ex2(FAR ? y - ref : y);
+          };
           uint32_t w[8];
           float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
             const int t = 16 * c + i;
-            float p0 = ex2(fmaf(__uint_as_float(x[i]), f, off)), p1 = ex2(fmaf(__uint_as_float(x[i + 1]), f, off));
+            float p0 = weight(x[i]), p1 = weight(x[i + 1]);
             if (M && (t > lim || t <= low)) p0 = 0.f;
             if (M && (t + 1 > lim || t + 1 <= low)) p1 = 0.f;
             acc[i & 3] += p0;
@@ -312,8 +324,9 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
         }
         tmem_ld_wait();
       };
-      if (__any_sync(0xffffffffu, lim < AT_T - 1 || low >= 0)) block(std::true_type{});
-      else block(std::false_type{});
+      if (!__any_sync(0xffffffffu, far || lim < AT_T - 1 || low >= 0)) block(std::false_type{}, std::false_type{});
+      else if (!__any_sync(0xffffffffu, far)) block(std::true_type{}, std::false_type{});
+      else block(std::true_type{}, std::true_type{});
       if (failed) break;
       // (block j - 4's have been read: the product of block j - 2, which p_free has told of, waited for the output of block j - 3)
       max_s[j & 3][tl] = bm;

@@ -141,3 +141,10 @@ HUGE = [1e6, 1e8, 3e8, 1e9, 1e20, 1e32]
 @pytest.mark.parametrize("sign", [-1.0, 1.0])
 def test_attend_huge_scores(torch, corun, G, hd, n, scale, sign):
     _one_token_takes_all(torch, corun, G, hd, n, scale, sign)
+
+
+@pytest.mark.parametrize("G,hd,n", [(8, 128, 9), (4, 64, 20)])
+@pytest.mark.parametrize("scale", HUGE)
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_chunk_huge_scores(torch, corun, G, hd, n, scale, sign):
+    _one_token_takes_all(torch, corun, G, hd, n, scale, sign)
