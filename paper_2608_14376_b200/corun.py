@@ -916,14 +916,16 @@ class Kv8Attention:
         oh = _heads(out, (n, n_q, hd), dt, dev, "out")
         r = cache._rows(ctx, block_table, cu, n)
         m = cache._mass(mass, block_table)
-        max_new = self.max_new if cu is not None else 1
+        max_new = max(min(self.max_new, n), 1) if cu is not None else 1   # (no row has more tokens than the call)
         if window >> 31:                                        # beyond 32 bits: wider than any cache, as all of 2^30 and above, or refused
             window = 0 if window > 0 else -1
         key = (n, max_new, m is not None)
         n_ws = self._bytes.get(key)
         if n_ws is None:
             n_ws = self._bytes[key] = lib().corun_kv8_attend_bytes(rows, n, max_new, n_q, n_kv, hd, block, max_blocks, int(key[2]))
-        # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph
+        # a workspace of the call's own: torch hands its memory out again in stream order, and to no other captured graph; the last
+        # call's may be this one's
+        self._last = None
         ws = T.empty(max(n_ws, 1), dtype=T.uint8, device=dev)
         _launch(lib().corun_kv8_attend, "corun_kv8_attend", dev, cache._c, r, max_new, qh, oh, code, n_q, scale, window, m, ws.data_ptr(), n_ws)
         # (a call without tokens has no status)

@@ -728,7 +728,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1) attend_kernel(const __grid_cons
         }
         if (a.mass && wq == 0 && lane < cols) a.ml[bg * a.cols + lane] = make_float2(m_run - 8.f, inv);
       } else {
-        const long long at = (bg * a.max_splits + x.split) * a.cols;
+        int step;
+        const long long at = part_at(a, x.b, x.first, x.n, x.g, x.split, G, step);
 #pragma unroll
         for (int c = 0; c < C; ++c)
           if (c < cols && has_dim) a.part_o[(at + c) * HD + d] = o[c];
@@ -764,11 +765,12 @@ __global__ void __launch_bounds__(32 * AT_PARTS) attend_combine_kernel(const __g
   const RowPlan r = row_plan(a.ctx[b], first, end, a, G);
   griddep_wait();
   if (r.ns <= 1 || col >= r.n * G) return;
-  const long long at = (long long)blockIdx.x * a.max_splits;
+  int cols;
+  const long long at = part_at(a, b, r.first, r.n, g, 0, G, cols) + col;
   const int parts = r.ns > AT_MANY ? AT_PARTS : AT_PARTS / 2;
   const int per = (r.ns + parts - 1) / parts, lo = q * per, hi = min(r.ns, lo + per);
-  const float *po = a.part_o + (at * a.cols + col) * HD + lane * W;
-  const long long step = (long long)a.cols * HD;
+  const float *po = a.part_o + at * HD + lane * W;
+  const long long step = (long long)cols * HD;
   auto load = [&](int s) {
     F f;
     if (W == 4) {
@@ -784,7 +786,7 @@ __global__ void __launch_bounds__(32 * AT_PARTS) attend_combine_kernel(const __g
 #pragma unroll
   for (int e = 0; e < AHEAD; ++e)
     if (lo + e < hi) x[e] = load(lo + e);
-  for (int s = threadIdx.x; s < r.ns; s += blockDim.x) sml[s] = __ldcg(a.part_ml + (at + s) * a.cols + col);
+  for (int s = threadIdx.x; s < r.ns; s += blockDim.x) sml[s] = __ldcg(a.part_ml + at + (long long)s * cols);
   __syncthreads();
   float M = AT_LOW;
   for (int s = lane; s < r.ns; s += 32) M = fmaxf(M, sml[s].x);
@@ -861,9 +863,10 @@ constexpr int at_columns(int wanted) { return wanted <= 4 ? 4 : wanted <= 8 ? 8 
 // Sizes of the workspace's parts, each on 256 bytes.
 struct AttendSpace {
   int cols, max_splits;
+  bool by_token;
   int64_t part_ml, part_o, ml, scores, score_tokens, bytes;
 };
-AttendSpace attend_space(int64_t B, int max_new, int n_q, int n_kv, int hd, int block, int max_blocks, bool mass) {
+AttendSpace attend_space(int64_t B, int64_t T, int max_new, int n_q, int n_kv, int hd, int block, int max_blocks, bool mass) {
   auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
   const int64_t G = n_q / n_kv, all = G * max_new;
   const int64_t reach_tiles = ((int64_t)max_blocks * block + AT_T - 1) / AT_T;
@@ -872,9 +875,11 @@ AttendSpace attend_space(int64_t B, int max_new, int n_q, int n_kv, int hd, int 
   s.max_splits = (int)(reach_tiles / AT_MIN_TILES);       // at_splits gives no more
   s.max_splits = s.max_splits < 1 ? 1 : s.max_splits > AT_SPLITS ? AT_SPLITS : s.max_splits;
   s.score_tokens = reach_tiles * AT_T;
+  s.by_token = T * G <= B * s.cols;
+  const int64_t parts = (s.by_token ? T * G : B * s.cols) * n_kv * s.max_splits;
   s.part_ml = AT_STATUS * 4;
-  s.part_o = s.part_ml + up(B * n_kv * s.max_splits * s.cols * 8);
-  s.ml = s.part_o + up(s.max_splits > 1 ? B * n_kv * s.max_splits * s.cols * hd * 4 : 0);
+  s.part_o = s.part_ml + up(parts * 8);
+  s.ml = s.part_o + up(s.max_splits > 1 ? parts * hd * 4 : 0);
   s.scores = s.ml + up(mass ? B * n_kv * s.cols * 8 : 0);
   s.bytes = s.scores + up(mass ? B * n_kv * s.score_tokens * s.cols * 4 : 0);
   return s;
@@ -925,7 +930,7 @@ extern "C" {
 int64_t corun_kv8_attend_bytes(int32_t B, int32_t T, int32_t max_new, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t block,
                                int32_t max_blocks, int32_t with_mass) {
   if (B < 1 || T < 1 || max_new < 1 || n_q < 1 || n_kv < 1 || n_q < n_kv || head_dim < 1 || block < 1 || max_blocks < 1) return 0;
-  return attend_space(B, max_new, n_q, n_kv, head_dim, block, max_blocks, with_mass != 0).bytes;
+  return attend_space(B, T, max_new, n_q, n_kv, head_dim, block, max_blocks, with_mass != 0).bytes;
 }
 
 int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, int32_t max_new, const corun_heads *q,
@@ -942,7 +947,7 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
     return CORUN_OK;
   }
   if (!q->p || !out->p || !heads_on_16(*q, dtype) || !heads_on_16(*out, dtype) || !ws || !aligned_to(ws, 256)) return CORUN_EINVAL;
-  const AttendSpace s = attend_space(rows->B, max_new, n_q, cache->n_kv, cache->head_dim, cache->block, rows->max_blocks, mass != nullptr);
+  const AttendSpace s = attend_space(rows->B, rows->T, max_new, n_q, cache->n_kv, cache->head_dim, cache->block, rows->max_blocks, mass != nullptr);
   if (ws_bytes < s.bytes) return CORUN_EINVAL;
   int dev = 0, sms = 0;
   cudaError_t ce = device_sms(&dev, &sms);
@@ -951,7 +956,7 @@ int corun_kv8_attend(const corun_kv8_cache *cache, const corun_kv8_rows *rows, i
   int rc = tma_encode_kv8(&tm, cache->pool, (unsigned long long)cache->pages, cache->n_kv, cache->block, cache->head_dim, 2);
   if (rc != CORUN_OK) return rc;
   char *w = (char *)ws;
-  const AttendArgs a{cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new, window < (1 << 30) ? window : 0, s.cols, s.max_splits, sms,
+  const AttendArgs a{cache->exps, cache->pages, cache->block, cache->n_kv, n_q, rows->B, rows->T, rows->max_blocks, max_new, window < (1 << 30) ? window : 0, s.cols, s.max_splits, sms, s.by_token,
                      rows->block_table, rows->ctx, rows->cu, q->p, out->p, q->token_stride, q->head_stride, out->token_stride, out->head_stride,
                      scale * 1.4426950408889634f, mass, (int *)w, (float2 *)(w + s.part_ml), (float *)(w + s.part_o), (float2 *)(w + s.ml),
                      (float *)(w + s.scores), s.score_tokens};

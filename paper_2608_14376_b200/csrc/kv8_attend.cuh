@@ -16,6 +16,7 @@ struct AttendArgs {
   const int8_t *exps;
   long long pages;
   int block, n_kv, n_q, B, T, max_blocks, max_new, window, cols, max_splits, sms;   // cols: columns per (row, key head) in the workspace
+  bool by_token;      // partial results: the row's place goes by its first token, not by its number
   const int *block_table, *ctx, *cu;
   const void *q;
   void *out;
@@ -23,8 +24,8 @@ struct AttendArgs {
   float scale_log2e;
   float *mass;
   int *status;
-  float2 *part_ml;    // [B][n_kv][max_splits][cols]: frame, sum
-  float *part_o;      // [B][n_kv][max_splits][cols][hd]
+  float2 *part_ml;    // a row's [n_kv][max_splits][columns] (part_at): frame, sum
+  float *part_o;      // the same, hd values each
   float2 *ml;         // [B][n_kv][cols]: frame, 1 / sum (with mass)
   float *scores;      // [B][n_kv][tokens padded to tiles][cols] (with mass)
   long long score_tokens;
@@ -35,6 +36,12 @@ struct AttendArgs {
 __device__ __forceinline__ bool at_row_ok(int c, int first, int end, const AttendArgs &a) {
   const int n = end - first;
   return c > 0 && (long long)c <= (long long)a.max_blocks * a.block && first >= 0 && end > first && n <= a.max_new && end <= a.T;
+}
+// Where the partial results of a row's split begin, and how many columns lie between two splits.  A row's columns are its tokens' times
+// G, so a call's rows together need no more than T * G, which is less than B times the largest row's where few rows bring many tokens.
+__device__ __forceinline__ long long part_at(const AttendArgs &a, int b, int first, int n, int g, int split, int G, int &cols) {
+  cols = a.by_token ? n * G : a.cols;
+  return (long long)(a.by_token ? first * G : b * a.cols) * (a.n_kv * a.max_splits) + (long long)(g * a.max_splits + split) * cols;
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;

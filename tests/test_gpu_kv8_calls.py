@@ -108,6 +108,23 @@ def test_windows_beyond_the_cache(torch, corun, window):
         att.run(q, s.cache, ctx, s.t_table, 0.1, window=-window)
 
 
+def test_workspace_is_held_once(torch, corun):
+    """Between two calls of an object there is one workspace, while the second runs there is no more than one."""
+    s = Setup(torch, corun, [3000] * 4, 4, 128, 16, seed=6)
+    q, ctx = _decode_call(torch, s, 32), _i32(torch, [3000] * 4)
+    out = torch.zeros_like(q)
+    att = corun.Kv8Attention(4, 32, 4, 128, s.max_blocks)
+    att.run(q, s.cache, ctx, s.t_table, 0.1, out=out)
+    att.sync()
+    held = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    att.run(q, s.cache, ctx, s.t_table, 0.1, out=out)
+    att.sync()
+    from paper_2608_14376_b200.corun import lib
+    size = lib().corun_kv8_attend_bytes(4, 4, 1, 32, 4, 128, 16, s.max_blocks, 0)
+    assert torch.cuda.memory_allocated() <= held and torch.cuda.max_memory_allocated() < held + size // 2
+
+
 # ---------------------------------------------------------------- numbers
 
 def _one_token_takes_all(torch, corun, G, hd, n, scale, sign):

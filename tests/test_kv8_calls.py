@@ -51,3 +51,13 @@ def test_evict_refuses_counts_beyond_32_bits(sinks, recent):
     one, table = torch.ones(1, dtype=torch.int32), torch.zeros(1, 4, dtype=torch.int32)
     with pytest.raises(ValueError, match="sinks"):
         cache.evict(one, table, torch.zeros(1, 2, 64), one, 32, sinks=sinks, recent=recent)
+
+
+def test_workspace_goes_by_the_tokens_that_there_are(lib):
+    """A call's partial results: a column per token and query head, where rows times the most columns of a row would be more."""
+    need = lambda B, T, max_new: lib.corun_kv8_attend_bytes(B, T, max_new, 32, 8, 128, 16, 2048, 0)
+    splits = 128                                                # tables of 32768 tokens: 256 tiles of 128
+    part = lambda columns: 8 * splits * columns * (128 + 2) * 4  # a column's running output, frame and sum
+    for B, T, max_new, columns in ((512, 512, 1, 512 * 4), (512, 512 + 511, 512, 1023 * 4), (64, 64 + 63, 64, 127 * 4), (64, 4096, 4096, 64 * 32),
+                                   (3, 9, 5, 9 * 4), (1, 300, 300, 32)):
+        assert part(columns) <= need(B, T, max_new) <= part(columns) + 4096, (B, T, max_new)
