@@ -165,3 +165,103 @@ def test_attend_huge_scores(torch, corun, G, hd, n, scale, sign):
 @pytest.mark.parametrize("sign", [-1.0, 1.0])
 def test_chunk_huge_scores(torch, corun, G, hd, n, scale, sign):
     _one_token_takes_all(torch, corun, G, hd, n, scale, sign)
+
+
+# ---------------------------------------------------------------- append: layouts that are read value by value
+
+N_NEW, START = [1, 2, 5, 16, 35, 1, 17, 3], [0, 7, 14, 0, 9, 48, 16, 100]
+
+
+def _off_16(torch, t):
+    """The same values in a layout whose heads do not start on 16 bytes."""
+    big = torch.empty(*t.shape[:-1], t.shape[-1] + 1, dtype=t.dtype, device=t.device)
+    big[..., 1:] = t
+    return big[..., 1:]
+
+
+def _append_case(torch, corun, hd, n_kv, G, dtype, seed):
+    dt = getattr(torch, dtype)
+    ctx = [a + b for a, b in zip(START, N_NEW)]
+    ctx[1] = 0
+    s = Setup(torch, corun, ctx, n_kv, hd, 16, seed=seed)
+    T = sum(N_NEW)
+    scale = 10.0 ** s.rng.uniform(-3, 3, (T, (G + 2) * n_kv, 1))
+    x = torch.tensor(s.rng.standard_normal((T, (G + 2) * n_kv, hd)) * scale).clamp(-6e4, 6e4).to(dt).cuda()
+    q, k, v = (t.contiguous() for t in x.split([G * n_kv, n_kv, n_kv], 1))
+    pos = s.rng.integers(0, 100000, T).astype(np.int32)
+    return s, ctx, q, k, v, pos, _i32(torch, np.concatenate([[0], np.cumsum(N_NEW)]))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("hd,n_kv,G", [(128, 2, 3), (64, 3, 1)])
+@pytest.mark.parametrize("rot,interleaved", [(6, False), (6, True), (20, False), (36, True), (36, False), (62, False), (64, True), (64, False), (0, False)])
+@pytest.mark.parametrize("off", [False, True])
+def test_append_value_by_value(torch, corun, dtype, hd, n_kv, G, rot, interleaved, off):
+    """Rotated parts that are no whole pieces of 16 bytes and heads that do not start on 16 bytes, queries in place."""
+    s, ctx, q, k, v, pos, cu = _append_case(torch, corun, hd, n_kv, G, dtype, seed=rot + hd)
+    rope = corun.Rope(rot, theta=1e6, interleaved=interleaved) if rot else None
+    # the same call on a copy of the cache through aligned tensors: the same bytes
+    other = corun.Kv8Cache(s.cache.pages, n_kv, hd, 16, pool=s.cache.pool.clone(), exps=s.cache.exps.clone())
+    args = dict(cu=cu, positions=_i32(torch, pos), rope=rope)
+    q_want = other.append(k, v, _i32(torch, ctx), s.t_table, q=q, q_out=torch.full_like(q, 9.0), **args)
+    if off:
+        qi, ki, vi = (_off_16(torch, t) for t in (q, k, v))
+    else:
+        qi, ki, vi = q.clone(), k, v
+    mass = torch.full((len(ctx), n_kv, s.max_blocks * 16), 3.0, device="cuda")
+    assert s.cache.append(ki, vi, _i32(torch, ctx), s.t_table, q=qi, q_out=qi, mass=mass, **args) is qi
+    live = torch.tensor(np.repeat(np.array(ctx) > 0, N_NEW), device="cuda")
+    assert torch.equal(qi[live], q_want[live]) and torch.equal(qi[~live], q[~live])
+    codes, exps = s.state()
+    assert np.array_equal(codes, other.pool.view(torch.uint8).cpu().numpy()) and np.array_equal(exps, other.exps.cpu().numpy())
+    # against 64 bits
+    f, m = ko.frequencies(rot, theta=1e6) if rot else (np.zeros(0), 1.0)
+    kr, qr = (ko.rotate(_np(t), pos, f, m, interleaved) for t in (k, q))
+    bound = _eps(torch, q.dtype) * np.abs(qr) + 8 * 2.0 ** -24 * np.abs(_np(q)).max(-1, keepdims=True) + (2.0 ** -25 if dtype == "float16" else 0)
+    alive = live.cpu().numpy()
+    assert np.all((np.abs(_np(qi) - qr) <= bound)[alive])
+    touched, at, first = np.zeros(codes.shape[0], bool), 0, s.codes
+    for b, n in enumerate(N_NEW):
+        if ctx[b] and n:
+            kk, vv = kr[at:at + n], _np(v)[at:at + n]
+            assert bool((mass[b, :, START[b]:ctx[b]] == 0).all()) and bool((mass[b, :, :START[b]] == 3).all()) and bool((mass[b, :, ctx[b]:] == 3).all())
+            for jb in range(START[b] // 16, (ctx[b] - 1) // 16 + 1):
+                pg, z0, z1 = s.table[b, jb], max(0, START[b] - jb * 16), min(16, ctx[b] - jb * 16)
+                touched[pg] = True
+                t0 = jb * 16 + z0 - START[b]
+                for kind, x in ((0, kk), (1, vv)):
+                    for h in range(n_kv):
+                        new, e = x[t0:t0 + z1 - z0, h], int(exps[pg, kind, h])
+                        slack = 8 * 2.0 ** -24 * np.abs(_np(k)[at + t0:at + t0 + z1 - z0, h]).max() if kind == 0 else 0.0
+                        old = int(s.exps[pg, kind, h]) if z0 else ko.E_MIN
+                        assert max(old, ko.exponent(max(np.abs(new).max() - slack, 0))) <= e <= max(old, ko.exponent(np.abs(new).max() + slack))
+                        _check_values(codes[pg, kind, h, z0:z1], new / 2.0 ** e, None, slack / 2.0 ** e)
+                        if z0:
+                            moved = ko.encode(ko.decode(first[pg, kind, h, :z0]) * 2.0 ** (old - e)) if e > old else first[pg, kind, h, :z0]
+                            assert np.array_equal(codes[pg, kind, h, :z0], moved)
+        at += n
+    assert np.array_equal(codes[~touched], s.codes[~touched]) and np.array_equal(exps[~touched], s.exps[~touched])
+
+
+# ---------------------------------------------------------------- chunks behind long contexts
+
+@pytest.mark.parametrize("n_kv,G,hd,block,dtype", [(2, 4, 128, 16, "bfloat16"), (1, 8, 64, 64, "float16"), (1, 5, 128, 32, "float16"), (2, 8, 64, 16, "bfloat16")])
+@pytest.mark.parametrize("window", [0, 1500])
+def test_chunks_behind_long_contexts(torch, corun, n_kv, G, hd, block, dtype, window):
+    """Rows of more than 32 columns over 20 to 70 blocks of 128 tokens, scales that differ from page to page by up to 2^12, beside a row of one token."""
+    ctx, n = [5000, 2600, 9000, 700], [50, 40, 9, 1]
+    s = Setup(torch, corun, ctx, n_kv, hd, block, seed=G + hd)
+    e = s.exps.astype(np.int32)
+    e[:, 0] += s.rng.integers(-6, 1, e[:, 0].shape)
+    e[:, 1] += s.rng.integers(-6, 7, e[:, 1].shape)
+    s.want.exps = e
+    s.cache.exps.copy_(torch.tensor(e.astype(np.int8)))
+    T = sum(n)
+    q = torch.tensor(s.rng.standard_normal((T, G * n_kv, hd)) * 0.3).to(getattr(torch, dtype)).cuda()
+    out = torch.full((T + 1, G * n_kv, hd), 5.0, dtype=q.dtype, device="cuda")
+    cu = _i32(torch, np.concatenate([[0], np.cumsum(n)]))
+    att = corun.Kv8Attention(4, G * n_kv, n_kv, hd, s.max_blocks, block, tokens=T, max_new=50)
+    att.run(q, s.cache, _i32(torch, ctx), s.t_table, hd ** -0.5, cu=cu, window=window, out=out[:T])
+    att.sync()
+    assert bool((out[T] == 5).all())
+    _check_attend(torch, s, q, out, None, None, ctx, n, window, hd ** -0.5)
