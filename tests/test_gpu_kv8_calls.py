@@ -167,6 +167,36 @@ def test_chunk_huge_scores(torch, corun, G, hd, n, scale, sign):
     _one_token_takes_all(torch, corun, G, hd, n, scale, sign)
 
 
+def _share_not_nearest(torch, corun, G, hd, n, seed):
+    """The share of fp16 outputs that are not the value nearest to the exact one, and what it may be.  Three e4m3 values of a weight: each
+    rounding leaves 2^-5 to 2^-4 of what it is given at most, evenly, so 2^-4.5 / sqrt(3) rms, and the third 1.7e-5 of the weight.  Values are
+    positive: an output is then off by r = 1.7e-5 |p v| / sum(p v) of itself, rms.  It is rounded the other way where the middle of two
+    neighbours (2^-11 of the value apart or more) lies in between: in r 2^11 of all cases, and twice that is allowed."""
+    c, n_kv = 40, 4
+    s = Setup(torch, corun, [c] * 3, n_kv, hd, 16, seed=seed)
+    codes = s.codes.copy()
+    codes[:, 1] = s.rng.integers(0x30, 0x78, codes[:, 1].shape)
+    s.cache.pool.copy_(torch.tensor(codes).cuda().view(torch.float8_e4m3fn))
+    s.want = ko.Cache(codes, s.exps)
+    q = torch.tensor(s.rng.standard_normal((3 * n, G * n_kv, hd)) * 0.2).half().cuda()
+    att = corun.Kv8Attention(3, G * n_kv, n_kv, hd, s.max_blocks, tokens=3 * n, max_new=n)
+    out = att.run(q, s.cache, _i32(torch, [c] * 3), s.t_table, hd ** -0.5, cu=_i32(torch, [0, n, 2 * n, 3 * n]))
+    att.sync()
+    off, r = [], []
+    for b in range(3):
+        k, v = s.want.values(s.table[b], c)
+        want, p, _, _ = ko.attend(_np(q)[b * n:(b + 1) * n], k, v, hd ** -0.5)
+        off.append(_np(out)[b * n:(b + 1) * n] != want.astype(np.float16).astype(np.float64))
+        r.append((2.0 ** -4.5 / 3 ** 0.5) ** 3 * np.sqrt(np.einsum("nhc,chd->nhd", p ** 2, np.repeat(v, G, 1) ** 2)) / want)
+    return np.mean(off), 2 * np.mean(r) * 2 ** 11
+
+
+@pytest.mark.parametrize("G,hd,n", [(4, 128, 1), (8, 64, 1), (2, 128, 2), (16, 128, 1), (32, 64, 1)])
+def test_attend_weights_keep_their_bits(torch, corun, G, hd, n):
+    off, most = _share_not_nearest(torch, corun, G, hd, n, seed=G + hd)
+    assert off <= most
+
+
 # ---------------------------------------------------------------- append: layouts that are read value by value
 
 N_NEW, START = [1, 2, 5, 16, 35, 1, 17, 3], [0, 7, 14, 0, 9, 48, 16, 100]
