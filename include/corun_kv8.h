@@ -73,7 +73,11 @@ int corun_kv8_append(const corun_kv8_cache *cache, const corun_kv8_rows *rows, c
  * A NaN among the values of a token reaches every query that sees the token, and may reach other queries of the same row and call.
  * n_q a multiple of n_kv, n_q / n_kv <= 32, B <= 512, scale > 0, T / (128 / (n_q / n_kv)) + B at most some 65000 (EINVAL beyond).  Queries and softmax weights enter the tensor cores as
  * sums of e4m3 values that hold 11 or more bits of them, but for what is below 2^-25 of the largest value of the query, or weight among 128
- * neighbouring tokens; scores, weights' sums and outputs are held in 32 bits.
+ * neighbouring tokens; scores, weights' sums and outputs are held in 32 bits
+ * (scores beyond 2^20 in magnitude so lose bits of their differences, and mass of its weights; outputs stay means of the values).
+ * A row with more than 32 columns (new tokens * n_q / n_kv) is not split over its cached tokens: one SM takes each of its tiles of 128
+ * columns and key head through all of them.  That is for chunks of prompts; a few tokens more than 32 columns hold behind a very long cache
+ * (100003 tokens, 8 heads a key head: 4 tokens 78 us, 5 tokens 2080) are faster in two calls.
  * Errors: EINVAL, ECUDA.  A bounded device-side wait that expires is recorded in the first 1024 bytes of ws: corun_kv8_sync waits for
  * the stream and returns ETIMEOUT in that case.  With T 0 corun_kv8_attend_bytes is 0 and ws may be NULL; where it has 1024 bytes or more,
  * those are cleared.  corun_kv8_sync is for a ws that has them.

@@ -31,12 +31,13 @@ typedef struct {
 typedef enum {
   CORUN_ROPE_PLAIN = 0,  /* f_i = theta^(-2i / rot_dim)                                                          */
   CORUN_ROPE_LINEAR = 1, /* f_i / factor                                                                         */
-  CORUN_ROPE_BASE = 2,   /* theta * factor^(rot_dim / (rot_dim - 2)) instead of theta                            */
-  CORUN_ROPE_PARTS = 3,  /* with d(n) = rot_dim ln(original_context / (2 pi n)) / (2 ln theta), the pair that turns n
+  CORUN_ROPE_BASE = 2,   /* theta * factor^(rot_dim / (rot_dim - 2)) instead of theta (known as NTK-aware)        */
+  CORUN_ROPE_PARTS = 3,  /* known as YaRN; low and high are its beta_slow and beta_fast.  With d(n) = rot_dim ln(original_context / (2 pi n)) / (2 ln theta), the pair that turns n
                             times in the trained context: r = clamp((i - first) / (last - first), 0, 1) from first =
                             max(floor d(high), 0) to last = min(ceil d(low), rot_dim - 1), f_i (1 - r + r / factor);
                             magnitude 0.1 ln(factor) + 1                                                         */
-  CORUN_ROPE_BANDS = 4   /* s = clamp((original_context f_i / (2 pi) - low) / (high - low), 0, 1),
+  CORUN_ROPE_BANDS = 4   /* by wavelength; low and high are called low_freq_factor and high_freq_factor in configurations that
+                            use it.  s = clamp((original_context f_i / (2 pi) - low) / (high - low), 0, 1),
                             f_i (s + (1 - s) / factor)                                                           */
 } corun_rope_scaling;
 

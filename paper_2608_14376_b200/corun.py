@@ -768,8 +768,9 @@ def _plain(t, shape, dtype, device, what):
 class Rope:
     """Rotary positions (``include/corun_rope.h``) of the first ``rot_dim`` values of every head.
 
-    ``interleaved``: pairs (2i, 2i + 1) instead of (i, i + rot_dim / 2); ``scaling``: one of ``ROPE_SCALINGS``, with
-    ``factor`` and, for "parts" and "bands", ``original_context``, ``low`` and ``high``; ``magnitude`` 0: the scaling's own."""
+    ``interleaved``: pairs (2i, 2i + 1) instead of (i, i + rot_dim / 2); ``scaling``: one of ``ROPE_SCALINGS`` ("base" is known as
+    NTK-aware, "parts" as YaRN, "bands" goes by wavelength), with ``factor`` and, for "parts" (beta_slow, beta_fast) and "bands"
+    (low_freq_factor, high_freq_factor), ``original_context``, ``low`` and ``high``; ``magnitude`` 0: the scaling's own."""
 
     def __init__(self, rot_dim: int, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0,
                  original_context: int = 0, low: float = 1.0, high: float = 32.0, magnitude: float = 0.0):

@@ -13,12 +13,17 @@
 //   the output of block j - 1, the keys of block j + 2, the values of block j + 1
 // in turn, beside the products.
 // A query row is brought to [256, 512) by a power of two before it is rounded to fp16: exact for bf16, and for fp16, but for values
-// some 2^-22 of the row's largest.
+// some 2^-22 of the row's largest.  One fp16 value of a weight is off by 2^-11 at most (or 2^-25 of the block's largest), an eighth of a bf16 output's
+// own rounding and as much as an fp16 output's; with a second value for the rest outputs are 6.6e-5 instead of 2.0e-4 from those in 32 bits, but
+// their errors against 64 bits the same in bf16, and the case below takes 270 us: the second products are two thirds of that.
 //
-// Measured on 3 rows of 200 to 700 new tokens behind up to 8192 cached ones (32 query, 8 key heads of 128, bf16): 247 us, 477 TFLOP/s; the
+// Measured on 3 rows of 200 to 700 new tokens behind up to 8192 cached ones (32 query, 8 key heads of 128, bf16): 249 us, 474 TFLOP/s; the
 // kernel for few columns took 1484.  A block takes 3300 to 3700 cycles, of which the products need 1024: the softmax (some 900 instructions a
 // warp and block, and a third of all issue slots), the output and the turning share the schedulers (62 % of issue slots, ALU pipe 42 %,
 // tensor pipe 27 %).  Turning with one fp16 tile of values and two of keys: 315 us; whichever product can go on first: 256.
+//
+// The cached tokens are not split: a row of few tiles behind a very long cache keeps few SMs busy (5 tokens x 8 heads, 4 key heads, 100003
+// cached tokens: 2080 us on 4 SMs, where kv8_attend.cu takes 78 for 4 tokens).
 //
 // Every reduction has one fixed order that depends on the row's own lengths only.  All waits are bounded.
 #include <math_constants.h>

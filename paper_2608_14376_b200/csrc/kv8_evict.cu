@@ -9,8 +9,9 @@
 // and goes through its tokens in order; what it writes in a round lies in front of everything that later rounds read, so
 // loads of the rounds to come are in flight while a round is stored, and stretches of dims do not meet.  No second copy of
 // the cache is needed.  Bound by bytes: the weights once (the digits' passes read shared memory), the tokens that stay once in, once out.
-// 16 rows of 6000 to 8192 tokens cut to 2048 (8 key heads of 128): listing 25 us and moving 36 us from a cold cache, 33 us in all where the
-// weights lie in L2 (22 at the copy rate).  The listing is a chain of passes with a CTA per (row, head) on 128 of 148 SMs; counting equal digits
+// 16 rows of 6000 to 8192 tokens cut to 2048 (8 key heads of 128): listing 25 us and moving 36 us from a cold cache (under the
+// profiler; 52 us in all without, 22 at the copy rate), and 33 us in all where the tokens that stay lie in order already, as behind an earlier
+// eviction: they are not moved again.  The listing is a chain of passes with a CTA per (row, head) on 128 of 148 SMs; counting equal digits
 // of a warp together took it to 34 us, 1024 threads changed nothing.  The move needs its loads spread over many warps: two rounds ahead
 // 36 us, four 36, eight 54; sources looked up page by page instead of listed 57; stretches of 32 bytes read 112 MB instead of 68 from DRAM.
 #include <atomic>
