@@ -258,14 +258,16 @@ __global__ void __launch_bounds__(CH_THREADS, 1) chunk_kernel(const __grid_const
     // ---------------- softmax: one thread per row; warps 0-3 the even blocks, warps 4-7 the odd ones
     const int pos = real ? pos0 + tl / G : -1;      // tokens up to pos are visible to this row
     const float qm = q_mul[tl];
+    // x f + (e_v - M) is rounded once where M was rounded before: they differ by up to |M| 2^-24, which is nothing while |M| stays below 2^20, but
+    // takes weights beyond fp16 from 2^28 on.  |x| is below 2^25: with keys' scales from here on, which a score might pass 2^20 with, the
+    // exponents are formed as M was.
+    const float far_from = real ? 0.03125f / qm : CUDART_INF_F;
     const int sb = warp >> 2;
     const uint32_t st = t_lane + (uint32_t)(sb * 128), pt = t_lane + L::P_COL + (uint32_t)(sb * 64);
     for (int j = sb; j < n_blocks; j += 2) {
       if (!wait_all(e_full[j % CH_EXPS], (uint32_t)(j / CH_EXPS))) break;
       const int8_t *ex = exps[j % CH_EXPS][0];
-      // x f + (e_v - M) is rounded once where M was rounded before: they differ by up to |M| 2^-24, which is nothing while |M| stays below 2^20,
-      // but takes weights beyond fp16 from 2^28 on.  |x| is below 2^25: where a score might pass 2^20, the exponents are formed as M was.
-      const bool far = k_top[j % CH_EXPS] * qm > 0.03125f;
+      const bool far = k_top[j % CH_EXPS] > far_from;
       if (!wait_all(s_full[sb], (uint32_t)(j >> 1))) break;
       tc_fence_after();
       const int lim = pos - (b0 + j) * AT_T, low = a.window ? lim - a.window : -1;   // tokens low + 1 .. lim of the block are visible
